@@ -21,6 +21,7 @@
  *  - Tensors are dense and contiguous, innermost dimension last:
  *      attention tensors  [B, heads, N, d]
  *      layer activations  [B, N, C]
+ *    Where a call takes an hla_view, the tensor may be strided.
  *  - Base addresses of tensors must be 16-byte aligned; index arrays 4-byte.
  *  - Element types: HLA_F32 (IEEE binary32) and HLA_BF16 (bfloat16 stored as
  *    uint16). Conversions to bf16 round to nearest even.
@@ -435,6 +436,53 @@ hla_status hla_qkv_proj_perm(const void *x, const void *w_qkv, const int32_t *or
 hla_status hla_out_proj_perm(const void *o, const void *w_proj, const int32_t *order,
                              void *y, int64_t B, int64_t N, int64_t heads, int64_t d,
                              int64_t c_out, hla_stream_t stream);
+
+/*
+ * A [B, heads, N, d] tensor with strides of its own (in elements; d contiguous), for
+ * rows that other data lies between: q inside a projection's [B, N, 3, heads, d], k
+ * and v inside [B, M, 2, heads, d]. ptr must be 16-byte aligned and every stride a
+ * multiple of 16 bytes and >= 0; the stride of a dimension of size 1 is not looked at.
+ * An input's stride may be 0 (one row or head for all). The rows of an output must not
+ * overlap each other (INVALID_ARG).
+ */
+typedef struct {
+  void *ptr;
+  int64_t batch, head, row;
+} hla_view;
+
+/*
+ * Rotary positions: every pair (x1, x2) of a row's first features is turned by the
+ * angle a = position * freqs[p] (radians):
+ *   y1 = magnitude * (x1 cos a - x2 sin a),  y2 = magnitude * (x2 cos a + x1 sin a);
+ * the features behind the pairs are copied. inverse != 0 turns by -a: it takes the
+ * gradient of the output to the gradient of the input, and undoes the call where
+ * magnitude is 1.
+ *  grid_w == 0: sequences. `pairs` pairs, the first 2 * pairs features.
+ *  grid_w >= 1: tokens of an image. A position is a row-major id of a grid of grid_w
+ *      columns; the first 2 * pairs features are turned by its row, the next
+ *      2 * pairs by its column (4 * pairs features in all). With pos =
+ *      hla_hilbert_perm's order, tokens in Hilbert order get their cells' rotations.
+ *  interleaved == 0: pair p is features (p, p + pairs) of its 2 * pairs features;
+ *  interleaved != 0: features (2p, 2p + 1).
+ * q: [B, heads, N, d], k: [B, kv_heads, N, d] or NULL (then kv_heads is ignored),
+ * turned in one launch; q_out, k_out: the same sizes. An output may be its input (the
+ * same pointer and strides); any other overlap of an output is INVALID_ARG.
+ * pos: device int32 [N] shared by the batch (pos_stride == 0), or [B, N] with
+ * pos_stride elements (>= N) between batch elements; any values (with a grid, ids
+ * >= 0; a negative one gives an unspecified angle). NULL: 0 .. N-1. It may not overlap
+ * an output. freqs: device float64 [pairs], 8-byte aligned; frequencies scaled for
+ * long contexts go in as they are.
+ * Angles are formed in float64 and reduced before they are rounded, so they
+ * are off by less than 2e-7 up to |position * frequency| = 2^28; the turn is fp32,
+ * rounded once to dtype.
+ * Supported: d * sizeof(dtype) a multiple of 16; B * N * d / 2 and B * (heads +
+ * kv_heads) up to 2^30; otherwise UNSUPPORTED.
+ */
+hla_status hla_rope(const hla_view *q, const hla_view *k, const hla_view *q_out,
+                    const hla_view *k_out, const int32_t *pos, int64_t pos_stride,
+                    const double *freqs, int64_t B, int64_t heads, int64_t kv_heads, int64_t N,
+                    int64_t d, int64_t pairs, int32_t grid_w, int32_t interleaved,
+                    int32_t inverse, float magnitude, hla_dtype dtype, hla_stream_t stream);
 
 /* Text of the last non-OK status returned on this thread ("" if none). */
 const char *hla_last_error(void);

@@ -15,12 +15,18 @@ fallback path.
     mask = build_block_mask(pattern, 128, 64, columns=True)   # + per-column lists
     dq, dk, dv = attn_bwd(qh, kh, vh, out, dout, lse, mask, scale)
 
+Around the attention, in a transformer block:
+
+    freqs, m = rope_freqs(d // 4)                         # rotary positions
+    q, k = rope(qh, freqs, k=kh, pos=order, grid_w=W)     # ... of the tokens' cells
+
 Patterns are given as any object with attributes kind, H, W, p0, p1 (kind is one
 of PATTERN_IDS), or as a tuple (kind, H, W, p0, p1).
 """
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import threading
 from typing import Optional, Tuple
@@ -31,7 +37,7 @@ __all__ = ["HLAError", "lib", "hilbert_perm", "gather", "scatter", "block_mask_d
            "build_block_mask", "BlockMask", "attn_fwd", "attn_fwd_perm", "attn_fwd_hilbert",
            "attn_fwd_rpb", "attn_bwd",
            "attn_bwd_perm",
-           "qkv_proj", "out_proj",
+           "qkv_proj", "out_proj", "rope", "rope_freqs",
            "PATTERN_IDS", "LIB_PATH", "EXPORTED"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhla.so")
@@ -57,7 +63,7 @@ EXPORTED = ("hla_hilbert_perm", "hla_gather", "hla_scatter", "hla_block_mask_dim
             "hla_attn_fwd_pattern", "hla_attn_fwd_hilbert", "hla_attn_fwd_rpb",
             "hla_attn_bwd", "hla_attn_bwd_perm", "hla_attn_bwd_noalloc",
             "hla_qkv_proj", "hla_out_proj", "hla_qkv_proj_perm", "hla_out_proj_perm",
-            "hla_last_error", "hla_version")
+            "hla_rope", "hla_last_error", "hla_version")
 
 
 class HLAError(RuntimeError):
@@ -85,6 +91,11 @@ class BlockMaskStruct(ctypes.Structure):
                 ("n_part_t", ctypes.c_void_p), ("part_idx_t", ctypes.c_void_p)]
 
 
+class View(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("batch", ctypes.c_int64), ("head", ctypes.c_int64),
+                ("row", ctypes.c_int64)]
+
+
 _lib = None
 _lib_lock = threading.Lock()
 
@@ -101,6 +112,7 @@ def lib() -> ctypes.CDLL:
             raise HLAError(-1, f"{LIB_PATH} is not built; run `python -m paper_2511_05832_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+        view = ctypes.POINTER(View)
         sigs = {
             "hla_hilbert_perm": [i32, i32, vp, vp, vp],
             "hla_gather": [vp, vp, vp, i64, i64, i64, i64, ctypes.c_int, vp],
@@ -128,6 +140,8 @@ def lib() -> ctypes.CDLL:
             "hla_out_proj": [vp, vp, vp, i64, i64, i64, i64, i64, vp],
             "hla_qkv_proj_perm": [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, vp],
             "hla_out_proj_perm": [vp, vp, vp, vp, i64, i64, i64, i64, i64, vp],
+            "hla_rope": [view, view, view, view, vp, i64, vp, i64, i64, i64, i64, i64, i64, i32, i32,
+                         i32, f32, ctypes.c_int, vp],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -625,3 +639,123 @@ def out_proj(o: torch.Tensor, w_proj: torch.Tensor, out: Optional[torch.Tensor] 
         _check(lib().hla_out_proj_perm(_ptr(o), _ptr(w_proj), _ptr(order), _ptr(out), B, N, Hh, d,
                                        c_out, _stream(o)))
     return out
+
+
+# ---------------------------------------------------------------------------
+# Operators around the attention. Tensors of one call are on one GPU; the call runs
+# there, on that GPU's current stream, whatever the current device is.
+
+def _call(t: torch.Tensor, fn, *args):
+    """fn(*args, stream) on t's device and its current stream."""
+    if t.get_device() == torch.cuda.current_device():
+        _check(fn(*args, _stream(t)))
+    else:
+        with torch.cuda.device(t.device):
+            _check(fn(*args, _stream(t)))
+
+
+def _rows(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> View:
+    """The view of a [B, heads, N, d] tensor whose rows are contiguous; ``like``: a
+    tensor that it shares device and dtype with."""
+    if not isinstance(t, torch.Tensor):
+        raise HLAError(HLA_ERR_INVALID_ARG, f"{name} must be a tensor")
+    if not t.is_cuda:
+        raise HLAError(HLA_ERR_INVALID_ARG, f"{name} must be on a GPU (got {t.device})")
+    if t.dim() != 4:
+        raise HLAError(HLA_ERR_INVALID_ARG, f"{name} must be [B, heads, N, d], got {tuple(t.shape)}")
+    if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device()):
+        raise HLAError(HLA_ERR_INVALID_ARG, f"{name} is {t.dtype} on {t.device}, expected {like.dtype} "
+                                            f"on {like.device}")
+    b, h, n, e = t.stride()
+    if e != 1 and t.shape[3] != 1:
+        raise HLAError(HLA_ERR_INVALID_ARG, f"{name}: the last dimension must be contiguous")
+    return View(t.data_ptr(), b, h, n)
+
+
+def _require_on(t: torch.Tensor, name: str, like: torch.Tensor, dtype: torch.dtype):
+    """A contiguous tensor of a type on the device of ``like``."""
+    _require(t, name)
+    if t.dtype != dtype or t.get_device() != like.get_device():
+        raise HLAError(HLA_ERR_INVALID_ARG, f"{name} must be {dtype} on {like.device} (got {t.dtype} on "
+                                            f"{t.device})")
+
+
+def rope_freqs(pairs: int, base: float = 10000.0, factor: float = 1.0, method: str = "linear",
+               length: Optional[int] = None, fast: float = 32.0, slow: float = 1.0,
+               device="cuda") -> Tuple[torch.Tensor, float]:
+    """Frequencies for ``rope``: (float64 [pairs] tensor of base^(-i / pairs), magnitude),
+    scaled for contexts ``factor`` times as long as the one trained on:
+
+    linear  every frequency divided by factor (position interpolation)
+    base    base raised by factor^(pairs / (pairs - 1)): the fastest pair unchanged, the
+            slowest divided by factor
+    parts   by the turns that a pair makes over the trained ``length`` (Peng et al.
+            2023, "YaRN"): pairs of more than ``fast`` turns unchanged, of less than
+            ``slow`` divided by factor, a linear ramp between; magnitude
+            0.1 ln(factor) + 1
+    """
+    if pairs < 1 or not base > 0 or not factor >= 1:
+        raise HLAError(HLA_ERR_INVALID_ARG, "rope_freqs needs pairs >= 1, base > 0, factor >= 1")
+    magnitude = 1.0
+    if method == "base" and pairs > 1:
+        base = base * factor ** (pairs / (pairs - 1))
+    freqs = [base ** (-i / pairs) for i in range(pairs)]
+    if method == "linear":
+        freqs = [f / factor for f in freqs]
+    elif method == "parts":
+        if length is None or length < 1 or not fast > slow:
+            raise HLAError(HLA_ERR_INVALID_ARG, "method 'parts' needs the trained length, and fast > slow")
+        for i, f in enumerate(freqs):
+            keep = min(1.0, max(0.0, (length * f / (2 * math.pi) - slow) / (fast - slow)))
+            freqs[i] = f * (keep + (1 - keep) / factor)
+        magnitude = 0.1 * math.log(factor) + 1.0
+    elif method != "base":
+        raise HLAError(HLA_ERR_INVALID_ARG, f"unknown method {method!r} (linear, base, parts)")
+    return torch.tensor(freqs, dtype=torch.float64, device=device), magnitude
+
+
+def rope(q: torch.Tensor, freqs: torch.Tensor, k: Optional[torch.Tensor] = None,
+         pos: Optional[torch.Tensor] = None, grid_w: int = 0, interleaved: bool = False,
+         magnitude: float = 1.0, inverse: bool = False, q_out: Optional[torch.Tensor] = None,
+         k_out: Optional[torch.Tensor] = None):
+    """Rotary positions on q [B, heads, N, d] and, in the same launch, k [B, kv_heads, N, d]
+    (hla_rope). Returns q_out, or (q_out, k_out) with k.
+
+    freqs: float64 [pairs] (``rope_freqs``). pos: int32 [N] or [B, N] (None: 0 .. N-1).
+    grid_w = 0: the first 2 * pairs features turn by the position. grid_w = W: positions
+    are row-major ids of an image W cells wide (``hilbert_perm``'s order for tokens in
+    Hilbert order); the first 2 * pairs features turn by the row, the next by the column.
+    interleaved: pairs (2p, 2p + 1) instead of (p, p + pairs). inverse: the other way, as
+    the gradients of q_out and k_out go. Tensors may be strided, rows contiguous; q_out
+    and k_out may be q and k."""
+    qv = _rows(q, "q")
+    code = _dtype_code(q)
+    B, heads, N, d = q.shape
+    _require_on(freqs, "freqs", q, torch.float64)
+    kv_heads = 0
+    if q_out is None:
+        q_out = q.new_empty(q.shape)
+    elif q_out.shape != q.shape:
+        raise HLAError(HLA_ERR_INVALID_ARG, "q_out must have q's shape")
+    kv = kov = None
+    if k is not None:
+        kv = _rows(k, "k", q)
+        kv_heads = k.shape[1]
+        if k.shape[0] != B or k.shape[2] != N or k.shape[3] != d:
+            raise HLAError(HLA_ERR_INVALID_ARG, f"k must be [{B}, kv_heads, {N}, {d}], got {tuple(k.shape)}")
+        if k_out is None:
+            k_out = k.new_empty(k.shape)
+        elif k_out.shape != k.shape:
+            raise HLAError(HLA_ERR_INVALID_ARG, "k_out must have k's shape")
+        kov = _rows(k_out, "k_out", q)
+    stride = 0
+    if pos is not None:
+        _require_on(pos, "pos", q, torch.int32)
+        if tuple(pos.shape) == (B, N):
+            stride = N
+        elif tuple(pos.shape) != (N,):
+            raise HLAError(HLA_ERR_INVALID_ARG, f"pos must be [{N}] or [{B}, {N}], got {tuple(pos.shape)}")
+    _call(q, lib().hla_rope, qv, kv, _rows(q_out, "q_out", q), kov, _ptr(pos), stride, _ptr(freqs), B,
+          heads, kv_heads, N, d, freqs.numel(), int(grid_w), int(interleaved), int(inverse),
+          float(magnitude), code)
+    return q_out if k is None else (q_out, k_out)

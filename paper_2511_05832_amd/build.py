@@ -23,9 +23,9 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libhla.so")
 ARCH = "gfx950"
 
-SOURCES = ["hla_api.cpp", "hilbert.hip", "permute.hip", "blockmask.hip",
+SOURCES = ["hla_api.cpp", "block_api.cpp", "hilbert.hip", "permute.hip", "blockmask.hip",
            "attn_bf16.hip", "attn_f32.hip", "attn_bwd_bf16.hip",
-           "attn_bwd_f32.hip", "proj.hip"]
+           "attn_bwd_f32.hip", "proj.hip", "rope.hip"]
 
 
 def hipcc() -> str:

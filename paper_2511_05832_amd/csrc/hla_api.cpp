@@ -7,7 +7,7 @@
 #include <mutex>
 #include <string>
 
-#include "hla_internal.h"
+#include "api_common.h"
 
 // Row statistics of the allocation-free backward (hla_attn_bwd_noalloc): two
 // floats per (b, h, row), up to kScratchRows rows. Every device the library
@@ -18,9 +18,9 @@
 constexpr int64_t kScratchRows = 1LL << 20;
 static __device__ __align__(256) float scratch[2 * kScratchRows];
 
-namespace {
+static thread_local std::string g_last_error;
 
-thread_local std::string g_last_error;
+namespace hla {
 
 hla_status fail(hla_status st, const char *fmt, ...) {
   char buf[512];
@@ -32,16 +32,11 @@ hla_status fail(hla_status st, const char *fmt, ...) {
   return st;
 }
 
-hla_status hip_status(hipError_t e, const char *what) {
-  if (e == hipSuccess) return HLA_OK;
-  return fail(HLA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
+}  // namespace hla
 
-bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-bool is_pow2(int64_t x) { return x > 0 && (x & (x - 1)) == 0; }
-int64_t dtype_size(hla_dtype dt) { return dt == HLA_F32 ? 4 : (dt == HLA_BF16 ? 2 : 0); }
+using namespace hla;
 
-constexpr int64_t kMaxI32 = 2147483647LL;
+namespace {
 
 hla_status check_pattern(const hla_pattern_desc *p) {
   if (!p) return fail(HLA_ERR_INVALID_ARG, "pattern descriptor is NULL");
@@ -89,17 +84,6 @@ hla_status check_tiles(int32_t tile_m, int32_t tile_n) {
       tile_n > 1024)
     return fail(HLA_ERR_UNSUPPORTED, "tiles %dx%d must be powers of two in [16, 1024]", tile_m, tile_n);
   return HLA_OK;
-}
-
-hla_status check_tensor_args(const void *a, const char *name) {
-  if (!a) return fail(HLA_ERR_INVALID_ARG, "%s is NULL", name);
-  if (!aligned(a, 16)) return fail(HLA_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
-  return HLA_OK;
-}
-
-bool overlaps(const void *a, int64_t na, const void *b, int64_t nb) {
-  const char *x = static_cast<const char *>(a), *y = static_cast<const char *>(b);
-  return x < y + nb && y < x + na;
 }
 
 constexpr int kMaxDevices = 64;

@@ -172,4 +172,23 @@ hipError_t launch_qkv_proj(const void *x, const void *w, const int32_t *order, v
 hipError_t launch_out_proj(const void *o, const void *w, const int32_t *order, void *y, int64_t B,
                            int64_t N, int64_t heads, int64_t d, int64_t c_out, hipStream_t s);
 
+// Rotary positions. Strides in elements.
+struct RopeTensor {
+  void *ptr;
+  int64_t batch, head, row;
+};
+struct RopeArgs {
+  RopeTensor in[2], out[2];   // q, k (k: no heads when absent)
+  const int32_t *pos;         // NULL: 0 .. N-1
+  int64_t pos_stride;         // between batch elements (0: shared)
+  const double *freqs;        // [pairs], radians per position
+  int32_t B, heads[2], N, d, pairs, axes, grid_w, interleaved, inverse;
+  float magnitude;
+  // set by the launcher
+  uint32_t total;             // threads
+  int32_t run, groups;        // slices per thread, groups of slices (per batch element where positions are)
+  FastDiv unit_div, n_div;
+};
+hipError_t launch_rope(RopeArgs a, hla_dtype dtype, hipStream_t s);
+
 }  // namespace hla
