@@ -484,6 +484,55 @@ hla_status hla_rope(const hla_view *q, const hla_view *k, const hla_view *q_out,
                     int64_t d, int64_t pairs, int32_t grid_w, int32_t interleaved,
                     int32_t inverse, float magnitude, hla_dtype dtype, hla_stream_t stream);
 
+/*
+ * Cross attention: queries against the states of another sequence (an encoder's, a
+ * text's, another image's), every query seeing the first lengths[b] states of its
+ * batch element:
+ *   out[b,h,i,:] = sum_j softmax_j(scale * <q_i, k_j> | j < lengths[b]) v_j
+ *   lse[b,h,i]   = ln sum_{j < lengths[b]} exp(scale * <q_i, k_j>)
+ * q, out: [B, heads, N, d]; k, v: [B, kv_heads, M, d], heads a multiple of kv_heads:
+ * query head h reads key head h / (heads / kv_heads). lse: float32 [B, heads, N],
+ * contiguous, or NULL. lengths: device int32 [B], 4-byte aligned, values taken into
+ * [0, M]; NULL: all M. With no state to see out = 0 and lse = -inf. States from
+ * lengths[b] on are not read into any result, whatever they hold.
+ * Any N, M >= 1: few rows (a decoder's single token) against many states split the
+ * states over workgroups.
+ * out may not overlap q, k, v, lengths or lse. bf16: products on bf16 matrix cores, softmax
+ * weights rounded to bf16 as operands, fp32 sums; f32: fp32 throughout.
+ * work: device workspace of at least the bytes that hla_cross_attn_workspace gives for
+ * these sizes on the current device, 16-byte aligned, overlapping no tensor; may be
+ * NULL where that is 0. A call's work is done with it when the call's work is done;
+ * calls whose work overlaps in time need one each.
+ * Supported: d in {32, 64}; row strides of k and v below 2^25 bytes; heads / kv_heads
+ * * N below 2^30; otherwise UNSUPPORTED.
+ */
+hla_status hla_cross_attn_fwd(const hla_view *q, const hla_view *k, const hla_view *v,
+                              const int32_t *lengths, const hla_view *out, float *lse, int64_t B,
+                              int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d,
+                              hla_dtype dtype, float scale, void *work, int64_t work_bytes,
+                              hla_stream_t stream);
+
+/*
+ * Its gradients for an upstream gradient dout (formulas as hla_attn_bwd's): out and lse
+ * are hla_cross_attn_fwd's results for the same arguments. dq: [B, heads, N, d]; dk,
+ * dv: [B, kv_heads, M, d], the sums over the heads that share a key head, 0 for states
+ * from lengths[b] on. Where k or v was broadcast (stride 0), dk and dv hold each
+ * element's own gradient and the caller sums. Outputs may not overlap each other or an
+ * input. No atomics: two calls give the same bits. lse is required; work as above (the
+ * backward always needs some).
+ */
+hla_status hla_cross_attn_bwd(const hla_view *q, const hla_view *k, const hla_view *v,
+                              const hla_view *out, const hla_view *dout, const float *lse,
+                              const int32_t *lengths, const hla_view *dq, const hla_view *dk,
+                              const hla_view *dv, int64_t B, int64_t heads, int64_t kv_heads,
+                              int64_t N, int64_t M, int64_t d, hla_dtype dtype, float scale,
+                              void *work, int64_t work_bytes, hla_stream_t stream);
+
+/* Bytes of workspace of the two calls (backward != 0: the second) on the current device. */
+hla_status hla_cross_attn_workspace(int64_t B, int64_t heads, int64_t kv_heads, int64_t N,
+                                    int64_t M, int64_t d, hla_dtype dtype, int32_t backward,
+                                    int64_t *bytes);
+
 /* Text of the last non-OK status returned on this thread ("" if none). */
 const char *hla_last_error(void);
 

@@ -19,6 +19,8 @@ Around the attention, in a transformer block:
 
     freqs, m = rope_freqs(d // 4)                         # rotary positions
     q, k = rope(qh, freqs, k=kh, pos=order, grid_w=W)     # ... of the tokens' cells
+    out, lse = cross_attn_fwd(q, ks, vs, lengths)         # states of another sequence
+    dq, dk, dv = cross_attn_bwd(q, ks, vs, out, dout, lse, lengths)
 
 Patterns are given as any object with attributes kind, H, W, p0, p1 (kind is one
 of PATTERN_IDS), or as a tuple (kind, H, W, p0, p1).
@@ -29,6 +31,7 @@ import ctypes
 import math
 import os
 import threading
+from contextlib import nullcontext
 from typing import Optional, Tuple
 
 import torch
@@ -37,7 +40,8 @@ __all__ = ["HLAError", "lib", "hilbert_perm", "gather", "scatter", "block_mask_d
            "build_block_mask", "BlockMask", "attn_fwd", "attn_fwd_perm", "attn_fwd_hilbert",
            "attn_fwd_rpb", "attn_bwd",
            "attn_bwd_perm",
-           "qkv_proj", "out_proj", "rope", "rope_freqs",
+           "qkv_proj", "out_proj", "rope", "rope_freqs", "cross_attn_fwd",
+           "cross_attn_bwd",
            "PATTERN_IDS", "LIB_PATH", "EXPORTED"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhla.so")
@@ -63,7 +67,8 @@ EXPORTED = ("hla_hilbert_perm", "hla_gather", "hla_scatter", "hla_block_mask_dim
             "hla_attn_fwd_pattern", "hla_attn_fwd_hilbert", "hla_attn_fwd_rpb",
             "hla_attn_bwd", "hla_attn_bwd_perm", "hla_attn_bwd_noalloc",
             "hla_qkv_proj", "hla_out_proj", "hla_qkv_proj_perm", "hla_out_proj_perm",
-            "hla_rope", "hla_last_error", "hla_version")
+            "hla_rope", "hla_cross_attn_fwd", "hla_cross_attn_bwd", "hla_cross_attn_workspace",
+            "hla_last_error", "hla_version")
 
 
 class HLAError(RuntimeError):
@@ -142,6 +147,12 @@ def lib() -> ctypes.CDLL:
             "hla_out_proj_perm": [vp, vp, vp, vp, i64, i64, i64, i64, i64, vp],
             "hla_rope": [view, view, view, view, vp, i64, vp, i64, i64, i64, i64, i64, i64, i32, i32,
                          i32, f32, ctypes.c_int, vp],
+            "hla_cross_attn_fwd": [view, view, view, vp, view, vp, i64, i64, i64, i64, i64, i64,
+                                   ctypes.c_int, f32, vp, i64, vp],
+            "hla_cross_attn_bwd": [view, view, view, view, view, vp, vp, view, view, view, i64, i64,
+                                   i64, i64, i64, i64, ctypes.c_int, f32, vp, i64, vp],
+            "hla_cross_attn_workspace": [i64, i64, i64, i64, i64, i64, ctypes.c_int, i32,
+                                         ctypes.POINTER(i64)],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -759,3 +770,88 @@ def rope(q: torch.Tensor, freqs: torch.Tensor, k: Optional[torch.Tensor] = None,
           heads, kv_heads, N, d, freqs.numel(), int(grid_w), int(interleaved), int(inverse),
           float(magnitude), code)
     return q_out if k is None else (q_out, k_out)
+
+
+def _cross_sizes(q, k, v, lengths):
+    """(views of q, k, v; (B, heads, kv_heads, N, M, d); dtype code) of a cross attention."""
+    views = _rows(q, "q"), _rows(k, "k", q), _rows(v, "v", q)
+    B, heads, N, d = q.shape
+    kv, M = k.shape[1], k.shape[2]
+    if k.shape[0] != B or k.shape[3] != d or v.shape != k.shape:
+        raise HLAError(HLA_ERR_INVALID_ARG, f"k and v must be [{B}, kv_heads, M, {d}] of one shape, got "
+                                            f"{tuple(k.shape)} and {tuple(v.shape)}")
+    if lengths is not None:
+        _require_on(lengths, "lengths", q, torch.int32)
+        if tuple(lengths.shape) != (B,):
+            raise HLAError(HLA_ERR_INVALID_ARG, f"lengths must be [{B}], got {tuple(lengths.shape)}")
+    return views, (B, heads, kv, N, M, d), _dtype_code(q)
+
+
+def _cross_work(q, sizes, code, backward):
+    """A workspace for one call (None where it needs none) and its bytes."""
+    n = ctypes.c_int64()
+    with torch.cuda.device(q.device) if q.get_device() != torch.cuda.current_device() else nullcontext():
+        _check(lib().hla_cross_attn_workspace(*sizes, code, backward, ctypes.byref(n)))
+    return (q.new_empty(n.value, dtype=torch.uint8) if n.value else None), n.value
+
+
+def _rows_like(t, name, like, shape):
+    """An output of a shape (default: a new tensor laid out as ``like``) and its view."""
+    if t is None:
+        t = torch.empty_like(like)
+    elif t.shape != shape:
+        raise HLAError(HLA_ERR_INVALID_ARG, f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    return t, _rows(t, name, like)
+
+
+def _lse_of(lse, q):
+    _require_on(lse, "lse", q, torch.float32)
+    if lse.shape != q.shape[:3]:
+        raise HLAError(HLA_ERR_INVALID_ARG, f"lse must be {tuple(q.shape[:3])}, got {tuple(lse.shape)}")
+    return lse
+
+
+def cross_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                   lengths: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                   out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                   with_lse: bool = True):
+    """Attention of q [B, heads, N, d] to the states of another sequence, k and v
+    [B, kv_heads, M, d] (hla_cross_attn_fwd). Returns (out, lse or None).
+
+    lengths: int32 [B], how many states of each batch element are seen (None: all M). A
+    query that sees none gets out = 0, lse = -inf. heads may be a multiple of kv_heads.
+    Tensors may be strided, rows contiguous: q from a token-wise projection is
+    ``linear(x, w).view(B, N, heads, d).transpose(1, 2)``; out is laid out like q."""
+    (qv, kv, vv), sizes, code = _cross_sizes(q, k, v, lengths)
+    out, ov = _rows_like(out, "out", q, q.shape)
+    if lse is not None:
+        _lse_of(lse, q)
+    elif with_lse:
+        lse = q.new_empty(q.shape[:3], dtype=torch.float32)
+    work, n = _cross_work(q, sizes, code, 0)
+    _call(q, lib().hla_cross_attn_fwd, qv, kv, vv, _ptr(lengths), ov, _ptr(lse), *sizes, code,
+          1.0 / float(q.shape[3]) ** 0.5 if scale is None else float(scale), _ptr(work), n)
+    return out, lse
+
+
+def cross_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                   dout: torch.Tensor, lse: torch.Tensor, lengths: Optional[torch.Tensor] = None,
+                   scale: Optional[float] = None, dq: Optional[torch.Tensor] = None,
+                   dk: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None):
+    """Gradients of ``cross_attn_fwd`` (hla_cross_attn_bwd): ``out`` and ``lse`` are its
+    results for these q, k, v, lengths and scale. Returns (dq, dk, dv); dk and dv are
+    summed over the heads that share a key head. The workspace of 8 bytes per row and
+    the splits' partial sums comes from torch's allocator."""
+    (qv, kv, vv), sizes, code = _cross_sizes(q, k, v, lengths)
+    for t, name in ((out, "out"), (dout, "dout")):
+        if not isinstance(t, torch.Tensor) or t.shape != q.shape:
+            raise HLAError(HLA_ERR_INVALID_ARG, f"{name} must be {tuple(q.shape)}")
+    _lse_of(lse, q)
+    dq, dqv = _rows_like(dq, "dq", q, q.shape)
+    dk, dkv = _rows_like(dk, "dk", k, k.shape)
+    dv, dvv = _rows_like(dv, "dv", v, v.shape)
+    work, n = _cross_work(q, sizes, code, 1)
+    _call(q, lib().hla_cross_attn_bwd, qv, kv, vv, _rows(out, "out", q), _rows(dout, "dout", q), _ptr(lse),
+          _ptr(lengths), dqv, dkv, dvv, *sizes, code,
+          1.0 / float(q.shape[3]) ** 0.5 if scale is None else float(scale), _ptr(work), n)
+    return dq, dk, dv

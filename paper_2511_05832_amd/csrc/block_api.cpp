@@ -3,6 +3,7 @@
 // before the first HIP call.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <utility>
 
 #include "api_common.h"
@@ -144,6 +145,195 @@ hla_status hla_rope(const hla_view *q, const hla_view *k, const hla_view *q_out,
   a.inverse = inverse != 0;
   a.magnitude = magnitude;
   return hip_status(launch_rope(a, dtype, (hipStream_t)stream), "hla_rope");
+}
+
+}  // extern "C"
+
+namespace {
+
+CrossStride cross_stride(const ViewShape &s) { return {s.v.batch, s.v.head, s.v.row}; }
+
+// Sizes of a cross attention, into the kernel's arguments.
+hla_status cross_sizes(int64_t B, int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d,
+                       hla_dtype dtype, bool backward, CrossArgs *a) {
+  if (!dtype_size(dtype)) return fail(HLA_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+  if (B <= 0 || heads <= 0 || kv_heads <= 0 || N <= 0 || M <= 0 || d <= 0)
+    return fail(HLA_ERR_INVALID_ARG, "sizes must be positive");
+  if (heads % kv_heads)
+    return fail(HLA_ERR_INVALID_ARG, "heads = %lld must be a multiple of kv_heads = %lld", (long long)heads, (long long)kv_heads);
+  if (d != 32 && d != 64) return fail(HLA_ERR_UNSUPPORTED, "head_dim %lld (supported: 32, 64)", (long long)d);
+  const int64_t G = heads / kv_heads, most = 1LL << 30;
+  if (B > most || heads > most || N > most || M > most || G > most / N || B > most / kv_heads)
+    return fail(HLA_ERR_UNSUPPORTED, "heads / kv_heads * N, M or B * kv_heads exceeds 2^30");
+  const int64_t bk = B * kv_heads, R = G * N;
+  // (every grid, in workgroups: below 2^31 with 64 rows or keys, or 256 threads, each)
+  if (R > (1LL << 36) / bk || M > (1LL << 36) / bk)
+    return fail(HLA_ERR_UNSUPPORTED, "B * heads * N or B * kv_heads * M exceeds 2^36");
+  a->B = (int32_t)B;
+  a->heads = (int32_t)heads;
+  a->kv = (int32_t)kv_heads;
+  a->G = (int32_t)G;
+  a->N = (int32_t)N;
+  a->M = (int32_t)M;
+  a->R = (int32_t)R;
+  a->Rp = (int32_t)((R + 127) / 128 * 128);
+  a->n_ktiles = (int32_t)((M + 63) / 64);
+  a->ndiv = make_fastdiv((uint32_t)N);
+  a->splits = backward ? cross_bwd_splits(*a) : cross_fwd_splits(*a);
+  return HLA_OK;
+}
+
+int64_t cross_bytes(const CrossArgs &a, int64_t d, bool backward) {
+  const int64_t bk = (int64_t)a.B * a.kv;
+  if (!backward) return a.splits == 1 ? 0 : bk * a.splits * a.R * (4 * d + 8);
+  return 8 * bk * a.Rp + (a.splits == 1 ? 0 : bk * a.splits * a.M * 8 * d);
+}
+
+hla_status cross_work(const CrossArgs &a, int64_t d, bool backward, const void *work, int64_t bytes) {
+  const int64_t need = cross_bytes(a, d, backward);
+  if (!need) return HLA_OK;
+  if (!work) return fail(HLA_ERR_INVALID_ARG, "work is NULL, %lld bytes are needed", (long long)need);
+  if (!aligned(work, 16)) return fail(HLA_ERR_INVALID_ARG, "work is not 16-byte aligned");
+  if (bytes < need)
+    return fail(HLA_ERR_INVALID_ARG, "work has %lld bytes, %lld are needed", (long long)bytes, (long long)need);
+  return HLA_OK;
+}
+
+hla_status cross_scale(float scale, CrossArgs *a) {
+  if (!(scale > 0.f) || scale > 1e30f) return fail(HLA_ERR_INVALID_ARG, "scale must be positive and finite");
+  a->scale = scale;
+  a->scale_log2 = (float)((double)scale * 1.4426950408889634074);
+  return HLA_OK;
+}
+
+// Views (q, k, v first, outputs last): pointers and strides of each, and no output on
+// another view or on one of the plain ranges.
+struct Range {
+  const char *name;
+  const void *p;
+  int64_t bytes;
+};
+hla_status cross_views(ViewShape *t, int n_in, int n, std::initializer_list<Range> ranges) {
+  hla_status st;
+  for (int i = 0; i < n; ++i)
+    if ((st = check_view(t[i], i >= n_in)) != HLA_OK) return st;
+  for (int i = 1; i < 3; ++i)   // k, v
+    if (t[i].v.row * t[i].es >= (1 << 25))
+      return fail(HLA_ERR_UNSUPPORTED, "the rows of %s must lie less than 2^25 bytes apart", t[i].name);
+  for (int i = n_in; i < n; ++i)
+    for (int j = 0; j < i; ++j)
+      if (views_clash(t[i], t[j])) return fail(HLA_ERR_INVALID_ARG, "%s overlaps %s", t[i].name, t[j].name);
+  for (const Range &r : ranges)
+    for (int i = n_in; i < n; ++i)
+      if (r.p && r.bytes && view_clash(t[i], r.p, r.bytes))
+        return fail(HLA_ERR_INVALID_ARG, "%s overlaps %s", t[i].name, r.name);
+  return HLA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+hla_status hla_cross_attn_workspace(int64_t B, int64_t heads, int64_t kv_heads, int64_t N,
+                                    int64_t M, int64_t d, hla_dtype dtype, int32_t backward,
+                                    int64_t *bytes) {
+  CrossArgs a;
+  if (!bytes) return fail(HLA_ERR_INVALID_ARG, "bytes is NULL");
+  hla_status st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, backward != 0, &a);
+  if (st == HLA_OK) *bytes = cross_bytes(a, d, backward != 0);
+  return st;
+}
+
+hla_status hla_cross_attn_fwd(const hla_view *q, const hla_view *k, const hla_view *v,
+                              const int32_t *lengths, const hla_view *out, float *lse, int64_t B,
+                              int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d,
+                              hla_dtype dtype, float scale, void *work, int64_t work_bytes,
+                              hla_stream_t stream) {
+  hla_status st;
+  CrossArgs a = {};
+  if (!q || !k || !v || !out) return fail(HLA_ERR_INVALID_ARG, "q, k, v or out is NULL");
+  if ((st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, false, &a)) != HLA_OK) return st;
+  if ((st = cross_scale(scale, &a)) != HLA_OK) return st;
+  if (lse && !aligned(lse, 4)) return fail(HLA_ERR_INVALID_ARG, "lse is not 4-byte aligned");
+  if (lengths && !aligned(lengths, 4)) return fail(HLA_ERR_INVALID_ARG, "lengths is not 4-byte aligned");
+  const int64_t es = dtype_size(dtype), lse_bytes = lse ? B * heads * N * 4 : 0;
+  ViewShape t[4] = {{"q", *q, {B, heads, N}, d, es}, {"k", *k, {B, kv_heads, M}, d, es},
+                    {"v", *v, {B, kv_heads, M}, d, es}, {"out", *out, {B, heads, N}, d, es}};
+  const int64_t need = cross_bytes(a, d, false);
+  if ((st = cross_views(t, 3, 4, {{"lse", lse, lse_bytes}, {"lengths", lengths, B * 4}, {"work", work, need}})) != HLA_OK)
+    return st;
+  if ((st = cross_work(a, d, false, work, work_bytes)) != HLA_OK) return st;
+  for (int i = 0; i < 3; ++i) {
+    if (need && view_clash(t[i], work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps %s", t[i].name);
+    if (lse && view_clash(t[i], lse, lse_bytes)) return fail(HLA_ERR_INVALID_ARG, "lse overlaps %s", t[i].name);
+  }
+  if (lse && need && overlaps(lse, lse_bytes, work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps lse");
+  if (lse && lengths && overlaps(lse, lse_bytes, lengths, B * 4)) return fail(HLA_ERR_INVALID_ARG, "lse overlaps lengths");
+  if (lengths && need && overlaps(lengths, B * 4, work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps lengths");
+  a.q = t[0].v.ptr;
+  a.k = t[1].v.ptr;
+  a.v = t[2].v.ptr;
+  a.out = t[3].v.ptr;
+  a.qs = cross_stride(t[0]);
+  a.ks = cross_stride(t[1]);
+  a.vs = cross_stride(t[2]);
+  a.os = cross_stride(t[3]);
+  a.lse = lse;
+  a.lengths = lengths;
+  if (a.splits > 1) {
+    a.part = static_cast<float *>(work);
+    a.part_ml = reinterpret_cast<float2 *>(a.part + (int64_t)a.B * a.kv * a.splits * a.R * d);
+  }
+  return hip_status(launch_cross_fwd(a, (int)d, dtype, (hipStream_t)stream), "hla_cross_attn_fwd");
+}
+
+hla_status hla_cross_attn_bwd(const hla_view *q, const hla_view *k, const hla_view *v,
+                              const hla_view *out, const hla_view *dout, const float *lse,
+                              const int32_t *lengths, const hla_view *dq, const hla_view *dk,
+                              const hla_view *dv, int64_t B, int64_t heads, int64_t kv_heads,
+                              int64_t N, int64_t M, int64_t d, hla_dtype dtype, float scale,
+                              void *work, int64_t work_bytes, hla_stream_t stream) {
+  hla_status st;
+  CrossArgs a = {};
+  if (!q || !k || !v || !out || !dout || !dq || !dk || !dv) return fail(HLA_ERR_INVALID_ARG, "a tensor is NULL");
+  if ((st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, true, &a)) != HLA_OK) return st;
+  if ((st = cross_scale(scale, &a)) != HLA_OK) return st;
+  if (!lse) return fail(HLA_ERR_INVALID_ARG, "lse is NULL");
+  if (!aligned(lse, 4)) return fail(HLA_ERR_INVALID_ARG, "lse is not 4-byte aligned");
+  if (lengths && !aligned(lengths, 4)) return fail(HLA_ERR_INVALID_ARG, "lengths is not 4-byte aligned");
+  const int64_t es = dtype_size(dtype), lse_bytes = B * heads * N * 4, need = cross_bytes(a, d, true);
+  ViewShape t[8] = {{"q", *q, {B, heads, N}, d, es},       {"k", *k, {B, kv_heads, M}, d, es},
+                    {"v", *v, {B, kv_heads, M}, d, es},    {"out", *out, {B, heads, N}, d, es},
+                    {"dout", *dout, {B, heads, N}, d, es}, {"dq", *dq, {B, heads, N}, d, es},
+                    {"dk", *dk, {B, kv_heads, M}, d, es},  {"dv", *dv, {B, kv_heads, M}, d, es}};
+  if ((st = cross_views(t, 5, 8, {{"lse", lse, lse_bytes}, {"lengths", lengths, B * 4}, {"work", work, need}})) != HLA_OK)
+    return st;
+  if ((st = cross_work(a, d, true, work, work_bytes)) != HLA_OK) return st;
+  for (int i = 0; i < 5; ++i)
+    if (view_clash(t[i], work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps %s", t[i].name);
+  if (overlaps(lse, lse_bytes, work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps lse");
+  if (lengths && overlaps(lengths, B * 4, work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps lengths");
+  a.q = t[0].v.ptr;
+  a.k = t[1].v.ptr;
+  a.v = t[2].v.ptr;
+  a.out = t[3].v.ptr;
+  a.dout = t[4].v.ptr;
+  a.dq = t[5].v.ptr;
+  a.dk = t[6].v.ptr;
+  a.dv = t[7].v.ptr;
+  a.qs = cross_stride(t[0]);
+  a.ks = cross_stride(t[1]);
+  a.vs = cross_stride(t[2]);
+  a.os = cross_stride(t[3]);
+  a.gs = cross_stride(t[4]);
+  a.dqs = cross_stride(t[5]);
+  a.dks = cross_stride(t[6]);
+  a.dvs = cross_stride(t[7]);
+  a.lse = const_cast<float *>(lse);
+  a.lengths = lengths;
+  a.stats = static_cast<float *>(work);
+  a.part = a.stats + 2 * (int64_t)a.B * a.kv * a.Rp;
+  return hip_status(launch_cross_bwd(a, (int)d, dtype, (hipStream_t)stream), "hla_cross_attn_bwd");
 }
 
 }  // extern "C"

@@ -191,4 +191,28 @@ struct RopeArgs {
 };
 hipError_t launch_rope(RopeArgs a, hla_dtype dtype, hipStream_t s);
 
+// Cross attention. Row r of a (batch, key head) pair is query r % N of head
+// kvh * G + r / N. Strides in elements.
+struct CrossStride {
+  int64_t batch, head, row;
+};
+struct CrossArgs {
+  const void *q, *k, *v, *dout;
+  void *out, *dq, *dk, *dv;    // (out: read by the backward)
+  CrossStride qs, ks, vs, os, gs, dqs, dks, dvs;
+  float *lse;                  // forward: written, or NULL; backward: read
+  const int32_t *lengths;      // [B], or NULL: all M keys are seen
+  float *stats;                // backward: lse log2 e of B * kv lists of Rp rows, then -delta of them
+  float *part;                 // partial sums of the splits
+  float2 *part_ml;             // forward: their maxima and sums
+  int32_t B, heads, kv, G, N, M, R, Rp, n_ktiles, splits;
+  int32_t n_rtiles;            // set by the launchers
+  FastDiv ndiv;                // division by N
+  float scale, scale_log2;
+};
+int cross_fwd_splits(const CrossArgs &a);   // from B, kv, R, M
+int cross_bwd_splits(const CrossArgs &a);
+hipError_t launch_cross_fwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s);
+hipError_t launch_cross_bwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s);
+
 }  // namespace hla
