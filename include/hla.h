@@ -533,6 +533,54 @@ hla_status hla_cross_attn_workspace(int64_t B, int64_t heads, int64_t kv_heads, 
                                     int64_t M, int64_t d, hla_dtype dtype, int32_t backward,
                                     int64_t *bytes);
 
+/*
+ * Token-wise linear layer with bias, activation and residual in its epilogue:
+ *   z = x W^T + bias,  y = act(z) + residual
+ * x: [T, K], w: [F, K] (row f is output feature f), bias: [F] or NULL, residual:
+ * [T, F] or NULL, y: [T, F], all of dtype, contiguous. pre: [T, F] or NULL, receives z
+ * (rounded to dtype), which the backward of an activation needs. residual may be y
+ * (the same address); other overlaps of y or pre are INVALID_ARG.
+ * HLA_ACT_GELU is z Phi(z); HLA_ACT_GELU_TANH its tanh form, z / 2 (1 + tanh(sqrt(2 /
+ * pi) (z + 0.044715 z^3))); HLA_ACT_SILU z / (1 + e^-z).
+ * bf16: products on bf16 matrix cores, everything up to y in fp32, rounded once; f32:
+ * fp32 throughout.
+ * Any T >= 1; K and F multiples of 8 (bf16) or 4 (f32), below 2^20; T up to 2^30,
+ * T * max(K, F) up to 2^42; otherwise UNSUPPORTED.
+ */
+typedef enum {
+  HLA_ACT_NONE = 0,
+  HLA_ACT_RELU = 1,
+  HLA_ACT_GELU = 2,
+  HLA_ACT_GELU_TANH = 3,
+  HLA_ACT_SILU = 4
+} hla_act;
+
+hla_status hla_linear(const void *x, const void *w, const void *bias, const void *residual,
+                      hla_act act, void *y, void *pre, int64_t T, int64_t K, int64_t F,
+                      hla_dtype dtype, hla_stream_t stream);
+
+/*
+ * Its gradients for an upstream gradient dy of y (the residual's gradient is dy):
+ *   dz = dy act'(z),  dx = dz W,  dw = dz^T x,  db = sum_t dz
+ * pre: the forward's z (not read, may be NULL, with HLA_ACT_NONE). dx [T, K], dw
+ * [F, K], db [F]: each may be NULL to leave it out (not all three). x is read for dw, w
+ * for dx; either may be NULL where it is not read. Outputs may not overlap each other
+ * or an input. dz is rounded to dtype as the products' operand; sums are fp32, in a
+ * fixed order (no atomics), rounded once.
+ * work: device workspace of at least the bytes that hla_linear_workspace gives on the
+ * current device, 16-byte aligned, overlapping no tensor; may be NULL where that is 0.
+ * Calls whose work overlaps in time need one each. Other support as hla_linear.
+ */
+hla_status hla_linear_bwd(const void *x, const void *w, const void *pre, const void *dy,
+                          hla_act act, void *dx, void *dw, void *db, int64_t T, int64_t K,
+                          int64_t F, hla_dtype dtype, void *work, int64_t work_bytes,
+                          hla_stream_t stream);
+
+/* Bytes of workspace of hla_linear_bwd for all three gradients on the current device
+ * (a call that leaves some out needs no more). */
+hla_status hla_linear_workspace(int64_t T, int64_t K, int64_t F, hla_act act, hla_dtype dtype,
+                                int64_t *bytes);
+
 /* Text of the last non-OK status returned on this thread ("" if none). */
 const char *hla_last_error(void);
 

@@ -21,6 +21,8 @@ Around the attention, in a transformer block:
     q, k = rope(qh, freqs, k=kh, pos=order, grid_w=W)     # ... of the tokens' cells
     out, lse = cross_attn_fwd(q, ks, vs, lengths)         # states of another sequence
     dq, dk, dv = cross_attn_bwd(q, ks, vs, out, dout, lse, lengths)
+    y, pre = linear(x, w, b, act="gelu", with_pre=True)   # act(x W^T + b) [+ residual]
+    dx, dw, db = linear_bwd(x, w, dy, pre, act="gelu", with_bias=True)
 
 Patterns are given as any object with attributes kind, H, W, p0, p1 (kind is one
 of PATTERN_IDS), or as a tuple (kind, H, W, p0, p1).
@@ -41,7 +43,7 @@ __all__ = ["HLAError", "lib", "hilbert_perm", "gather", "scatter", "block_mask_d
            "attn_fwd_rpb", "attn_bwd",
            "attn_bwd_perm",
            "qkv_proj", "out_proj", "rope", "rope_freqs", "cross_attn_fwd",
-           "cross_attn_bwd",
+           "cross_attn_bwd", "linear", "linear_bwd", "ACTS",
            "PATTERN_IDS", "LIB_PATH", "EXPORTED"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhla.so")
@@ -58,6 +60,8 @@ PATTERN_IDS = {
 
 _ROWMAJOR_IDS = frozenset(i for n, i in PATTERN_IDS.items() if n.startswith("rowmajor"))
 
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
 HLA_OK, HLA_ERR_INVALID_ARG, HLA_ERR_UNSUPPORTED, HLA_ERR_HIP = 0, 1, 2, 3
 HLA_F32, HLA_BF16 = 0, 1
 HLA_WALK_AUTO, HLA_WALK_LISTS, HLA_WALK_PATCHES = 0, 1, 2
@@ -68,7 +72,7 @@ EXPORTED = ("hla_hilbert_perm", "hla_gather", "hla_scatter", "hla_block_mask_dim
             "hla_attn_bwd", "hla_attn_bwd_perm", "hla_attn_bwd_noalloc",
             "hla_qkv_proj", "hla_out_proj", "hla_qkv_proj_perm", "hla_out_proj_perm",
             "hla_rope", "hla_cross_attn_fwd", "hla_cross_attn_bwd", "hla_cross_attn_workspace",
-            "hla_last_error", "hla_version")
+            "hla_linear", "hla_linear_bwd", "hla_linear_workspace", "hla_last_error", "hla_version")
 
 
 class HLAError(RuntimeError):
@@ -153,6 +157,10 @@ def lib() -> ctypes.CDLL:
                                    i64, i64, i64, i64, ctypes.c_int, f32, vp, i64, vp],
             "hla_cross_attn_workspace": [i64, i64, i64, i64, i64, i64, ctypes.c_int, i32,
                                          ctypes.POINTER(i64)],
+            "hla_linear": [vp, vp, vp, vp, ctypes.c_int, vp, vp, i64, i64, i64, ctypes.c_int, vp],
+            "hla_linear_bwd": [vp, vp, vp, vp, ctypes.c_int, vp, vp, vp, i64, i64, i64, ctypes.c_int,
+                               vp, i64, vp],
+            "hla_linear_workspace": [i64, i64, i64, ctypes.c_int, ctypes.c_int, ctypes.POINTER(i64)],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -855,3 +863,80 @@ def cross_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
           _ptr(lengths), dqv, dkv, dvv, *sizes, code,
           1.0 / float(q.shape[3]) ** 0.5 if scale is None else float(scale), _ptr(work), n)
     return dq, dk, dv
+
+
+def _act_code(act: str) -> int:
+    code = ACTS.get(act)
+    if code is None:
+        raise HLAError(HLA_ERR_INVALID_ARG, f"unknown activation {act!r} ({', '.join(ACTS)})")
+    return code
+
+
+def _linear_sizes(x, w):
+    """(T, K, F) of x [..., K] and w [F, K]."""
+    _require(x, "x")
+    _require_on(w, "w", x, x.dtype)
+    if x.dim() < 1 or w.dim() != 2 or w.shape[1] != x.shape[-1]:
+        raise HLAError(HLA_ERR_INVALID_ARG, f"x must be [..., K] and w [F, K], got {tuple(x.shape)} and "
+                                            f"{tuple(w.shape)}")
+    F, K = w.shape
+    return (x.numel() // K if K else 0), K, F
+
+
+def _shaped(t, name, like, shape):
+    """A given tensor of a shape (default: a new one) with the type and device of ``like``."""
+    if t is None:
+        return like.new_empty(shape)
+    _require_on(t, name, like, like.dtype)
+    if tuple(t.shape) != tuple(shape):
+        raise HLAError(HLA_ERR_INVALID_ARG, f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
+           residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+           pre: Optional[torch.Tensor] = None, with_pre: bool = False):
+    """y [..., F] = act(x W^T + bias) + residual for x [..., K], w [F, K] (hla_linear).
+    act: one of ACTS. Returns y, or (y, pre) when ``pre`` is given or ``with_pre`` asks
+    for it: the activation's argument, which ``linear_bwd`` takes. ``residual`` may be
+    ``out``."""
+    T, K, F = _linear_sizes(x, w)
+    code, act_code = _dtype_code(x), _act_code(act)
+    shape = (*x.shape[:-1], F)
+    if bias is not None:
+        _shaped(bias, "bias", x, (F,))
+    if residual is not None:
+        _shaped(residual, "residual", x, shape)
+    out = _shaped(out, "out", x, shape)
+    if with_pre or pre is not None:
+        pre = _shaped(pre, "pre", x, shape)
+    _call(x, lib().hla_linear, _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), act_code, _ptr(out),
+          _ptr(pre), T, K, F, code)
+    return out if pre is None else (out, pre)
+
+
+def linear_bwd(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, pre: Optional[torch.Tensor] = None,
+               act: str = "none", with_bias: bool = False, dx: Optional[torch.Tensor] = None,
+               dw: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None):
+    """Gradients of ``linear`` for dy [..., F] (hla_linear_bwd): (dx, dw, db), db None
+    unless ``with_bias`` asks for it or ``db`` is given. ``pre`` is the forward's; only
+    an activation needs it. The residual's gradient is dy itself."""
+    T, K, F = _linear_sizes(x, w)
+    code, act_code = _dtype_code(x), _act_code(act)
+    shape = (*x.shape[:-1], F)
+    if dy is None or (pre is None and act_code):
+        raise HLAError(HLA_ERR_INVALID_ARG, "linear_bwd needs dy, and pre with an activation")
+    _shaped(dy, "dy", x, shape)
+    if act_code:
+        _shaped(pre, "pre", x, shape)
+    dx = _shaped(dx, "dx", x, x.shape)
+    dw = _shaped(dw, "dw", x, w.shape)
+    if with_bias or db is not None:
+        db = _shaped(db, "db", x, (F,))
+    n = ctypes.c_int64()
+    with torch.cuda.device(x.device) if x.get_device() != torch.cuda.current_device() else nullcontext():
+        _check(lib().hla_linear_workspace(T, K, F, act_code, code, ctypes.byref(n)))
+    work = x.new_empty(n.value, dtype=torch.uint8) if n.value else None
+    _call(x, lib().hla_linear_bwd, _ptr(x), _ptr(w), _ptr(pre) if act_code else 0, _ptr(dy), act_code,
+          _ptr(dx), _ptr(dw), _ptr(db), T, K, F, code, _ptr(work), n.value)
+    return dx, dw, db

@@ -25,7 +25,8 @@ ARCH = "gfx950"
 
 SOURCES = ["hla_api.cpp", "block_api.cpp", "hilbert.hip", "permute.hip", "blockmask.hip",
            "attn_bf16.hip", "attn_f32.hip", "attn_bwd_bf16.hip",
-           "attn_bwd_f32.hip", "proj.hip", "rope.hip", "cross_attn.hip"]
+           "attn_bwd_f32.hip", "proj.hip", "rope.hip", "cross_attn.hip",
+           "linear.hip"]
 
 
 def hipcc() -> str:

@@ -337,3 +337,121 @@ hla_status hla_cross_attn_bwd(const hla_view *q, const hla_view *k, const hla_vi
 }
 
 }  // extern "C"
+
+namespace {
+
+struct Tensor {
+  const char *name;
+  const void *p;
+  int64_t bytes;
+};
+
+hla_status linear_sizes(int64_t T, int64_t K, int64_t F, hla_act act, hla_dtype dtype, LinearArgs *a) {
+  const int64_t es = dtype_size(dtype);
+  if (!es) return fail(HLA_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+  if (act < HLA_ACT_NONE || act > HLA_ACT_SILU) return fail(HLA_ERR_INVALID_ARG, "unknown activation %d", (int)act);
+  if (T <= 0 || K <= 0 || F <= 0) return fail(HLA_ERR_INVALID_ARG, "sizes must be positive");
+  if (K * es % 16 || F * es % 16)
+    return fail(HLA_ERR_UNSUPPORTED, "K = %lld and F = %lld must be multiples of %lld", (long long)K, (long long)F,
+                (long long)(16 / es));
+  if (T > (1LL << 30) || K >= (1 << 20) || F >= (1 << 20))
+    return fail(HLA_ERR_UNSUPPORTED, "T above 2^30, or K or F not below 2^20");
+  // (workgroups of the smallest tiles, and of the 16-feature ones)
+  if (((T + 63) / 64) * ((std::max(K, F) + 63) / 64) > (1LL << 30)) return fail(HLA_ERR_UNSUPPORTED, "T * max(K, F) above 2^42");
+  *a = {};
+  a->T = (int32_t)T;
+  a->K = (int32_t)K;
+  a->F = (int32_t)F;
+  a->act = act;
+  return HLA_OK;
+}
+
+// The inputs' and outputs' pointers, and no output on an input or another output. NULL
+// entries are left out.
+hla_status linear_tensors(const Tensor *in, int ni, const Tensor *out, int no) {
+  hla_status st;
+  for (int i = 0; i < ni; ++i)
+    if (in[i].p && (st = check_tensor_args(in[i].p, in[i].name)) != HLA_OK) return st;
+  for (int i = 0; i < no; ++i) {
+    if (!out[i].p) continue;
+    if ((st = check_tensor_args(out[i].p, out[i].name)) != HLA_OK) return st;
+    for (int j = 0; j < ni; ++j)
+      if (in[j].p && overlaps(out[i].p, out[i].bytes, in[j].p, in[j].bytes))
+        return fail(HLA_ERR_INVALID_ARG, "%s overlaps %s", out[i].name, in[j].name);
+    for (int j = 0; j < i; ++j)
+      if (out[j].p && overlaps(out[i].p, out[i].bytes, out[j].p, out[j].bytes))
+        return fail(HLA_ERR_INVALID_ARG, "%s overlaps %s", out[i].name, out[j].name);
+  }
+  return HLA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+hla_status hla_linear(const void *x, const void *w, const void *bias, const void *residual,
+                      hla_act act, void *y, void *pre, int64_t T, int64_t K, int64_t F,
+                      hla_dtype dtype, hla_stream_t stream) {
+  LinearArgs a;
+  hla_status st = linear_sizes(T, K, F, act, dtype, &a);
+  if (st != HLA_OK) return st;
+  if (!x || !w || !y) return fail(HLA_ERR_INVALID_ARG, "%s is NULL", !x ? "x" : (!w ? "w" : "y"));
+  const int64_t es = dtype_size(dtype);
+  // (residual == y is allowed: each element is read before it is written, by one thread)
+  const Tensor in[4] = {{"x", x, T * K * es}, {"w", w, F * K * es}, {"bias", bias, F * es},
+                        {"residual", residual == y ? nullptr : residual, T * F * es}};
+  const Tensor out[2] = {{"y", y, T * F * es}, {"pre", pre, T * F * es}};
+  if ((st = linear_tensors(in, 4, out, 2)) != HLA_OK) return st;
+  a.x = x;
+  a.w = w;
+  a.bias = bias;
+  a.residual = residual;
+  a.y = y;
+  a.pre = pre;
+  return hip_status(launch_linear(a, dtype, (hipStream_t)stream), "hla_linear");
+}
+
+hla_status hla_linear_workspace(int64_t T, int64_t K, int64_t F, hla_act act, hla_dtype dtype,
+                                int64_t *bytes) {
+  LinearArgs a;
+  if (!bytes) return fail(HLA_ERR_INVALID_ARG, "bytes is NULL");
+  hla_status st = linear_sizes(T, K, F, act, dtype, &a);
+  if (st != HLA_OK) return st;
+  a.dx = a.dw = a.db = bytes;   // (all of them; the addresses are not used)
+  *bytes = linear_work(a, (int)dtype_size(dtype)).bytes;
+  return HLA_OK;
+}
+
+hla_status hla_linear_bwd(const void *x, const void *w, const void *pre, const void *dy,
+                          hla_act act, void *dx, void *dw, void *db, int64_t T, int64_t K,
+                          int64_t F, hla_dtype dtype, void *work, int64_t work_bytes,
+                          hla_stream_t stream) {
+  LinearArgs a;
+  hla_status st = linear_sizes(T, K, F, act, dtype, &a);
+  if (st != HLA_OK) return st;
+  if (!dx && !dw && !db) return fail(HLA_ERR_INVALID_ARG, "dx, dw and db are all NULL");
+  if (!dy) return fail(HLA_ERR_INVALID_ARG, "dy is NULL");
+  if (dx && !w) return fail(HLA_ERR_INVALID_ARG, "w is NULL");
+  if (dw && !x) return fail(HLA_ERR_INVALID_ARG, "x is NULL");
+  if (act != HLA_ACT_NONE && !pre) return fail(HLA_ERR_INVALID_ARG, "pre is NULL");
+  if (act == HLA_ACT_NONE) pre = nullptr;
+  a.x = x;
+  a.w = w;
+  a.pre = const_cast<void *>(pre);
+  a.dy = dy;
+  a.dx = dx;
+  a.dw = dw;
+  a.db = db;
+  const int64_t es = dtype_size(dtype), need = linear_work(a, (int)es).bytes;
+  const Tensor in[4] = {{"x", x, T * K * es}, {"w", w, F * K * es}, {"pre", pre, T * F * es}, {"dy", dy, T * F * es}};
+  const Tensor out[4] = {{"dx", dx, T * K * es}, {"dw", dw, F * K * es}, {"db", db, F * es},
+                         {"work", need ? work : nullptr, need}};
+  if (need && !work) return fail(HLA_ERR_INVALID_ARG, "work is NULL, %lld bytes are needed", (long long)need);
+  if (work_bytes < need)
+    return fail(HLA_ERR_INVALID_ARG, "work has %lld bytes, %lld are needed", (long long)work_bytes, (long long)need);
+  if ((st = linear_tensors(in, 4, out, 4)) != HLA_OK) return st;
+  a.work = work;
+  return hip_status(launch_linear_bwd(a, dtype, (hipStream_t)stream), "hla_linear_bwd");
+}
+
+}  // extern "C"
