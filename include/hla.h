@@ -544,6 +544,11 @@ hla_status hla_cross_attn_workspace(int64_t B, int64_t heads, int64_t kv_heads, 
  * pi) (z + 0.044715 z^3))); HLA_ACT_SILU z / (1 + e^-z).
  * bf16: products on bf16 matrix cores, everything up to y in fp32, rounded once; f32:
  * fp32 throughout.
+ * work: device workspace, 16-byte aligned, overlapping no tensor, or NULL. With the bytes
+ * that hla_linear_workspace gives (0 up to 64 tokens) the contraction is split over
+ * workgroups where the results alone are too few to fill the GPU; with less it is not,
+ * which is slower and sums in another order. Calls whose work overlaps in time need one
+ * each.
  * Any T >= 1; K and F multiples of 8 (bf16) or 4 (f32), below 2^20; T up to 2^30,
  * T * max(K, F) up to 2^42; otherwise UNSUPPORTED.
  */
@@ -557,7 +562,7 @@ typedef enum {
 
 hla_status hla_linear(const void *x, const void *w, const void *bias, const void *residual,
                       hla_act act, void *y, void *pre, int64_t T, int64_t K, int64_t F,
-                      hla_dtype dtype, hla_stream_t stream);
+                      hla_dtype dtype, void *work, int64_t work_bytes, hla_stream_t stream);
 
 /*
  * Its gradients for an upstream gradient dy of y (the residual's gradient is dy):
@@ -576,10 +581,10 @@ hla_status hla_linear_bwd(const void *x, const void *w, const void *pre, const v
                           int64_t F, hla_dtype dtype, void *work, int64_t work_bytes,
                           hla_stream_t stream);
 
-/* Bytes of workspace of hla_linear_bwd for all three gradients on the current device
- * (a call that leaves some out needs no more). */
+/* Bytes of workspace of hla_linear (backward == 0) or hla_linear_bwd for all three
+ * gradients (a call that leaves some out needs no more), on the current device. */
 hla_status hla_linear_workspace(int64_t T, int64_t K, int64_t F, hla_act act, hla_dtype dtype,
-                                int64_t *bytes);
+                                int32_t backward, int64_t *bytes);
 
 /* Text of the last non-OK status returned on this thread ("" if none). */
 const char *hla_last_error(void);

@@ -157,10 +157,12 @@ def lib() -> ctypes.CDLL:
                                    i64, i64, i64, i64, ctypes.c_int, f32, vp, i64, vp],
             "hla_cross_attn_workspace": [i64, i64, i64, i64, i64, i64, ctypes.c_int, i32,
                                          ctypes.POINTER(i64)],
-            "hla_linear": [vp, vp, vp, vp, ctypes.c_int, vp, vp, i64, i64, i64, ctypes.c_int, vp],
+            "hla_linear": [vp, vp, vp, vp, ctypes.c_int, vp, vp, i64, i64, i64, ctypes.c_int, vp, i64,
+                           vp],
             "hla_linear_bwd": [vp, vp, vp, vp, ctypes.c_int, vp, vp, vp, i64, i64, i64, ctypes.c_int,
                                vp, i64, vp],
-            "hla_linear_workspace": [i64, i64, i64, ctypes.c_int, ctypes.c_int, ctypes.POINTER(i64)],
+            "hla_linear_workspace": [i64, i64, i64, ctypes.c_int, ctypes.c_int, i32,
+                                     ctypes.POINTER(i64)],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -893,6 +895,14 @@ def _shaped(t, name, like, shape):
     return t
 
 
+def _linear_work(x, T, K, F, act_code, code, backward):
+    """A workspace for one call (None where it needs none) and its bytes."""
+    n = ctypes.c_int64()
+    with torch.cuda.device(x.device) if x.get_device() != torch.cuda.current_device() else nullcontext():
+        _check(lib().hla_linear_workspace(T, K, F, act_code, code, backward, ctypes.byref(n)))
+    return (x.new_empty(n.value, dtype=torch.uint8) if n.value else None), n.value
+
+
 def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
            residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
            pre: Optional[torch.Tensor] = None, with_pre: bool = False):
@@ -910,8 +920,10 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     out = _shaped(out, "out", x, shape)
     if with_pre or pre is not None:
         pre = _shaped(pre, "pre", x, shape)
+    # (up to 64 tokens it needs none)
+    work, n = _linear_work(x, T, K, F, act_code, code, 0) if T > 64 else (None, 0)
     _call(x, lib().hla_linear, _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), act_code, _ptr(out),
-          _ptr(pre), T, K, F, code)
+          _ptr(pre), T, K, F, code, _ptr(work), n)
     return out if pre is None else (out, pre)
 
 
@@ -933,10 +945,7 @@ def linear_bwd(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, pre: Optional
     dw = _shaped(dw, "dw", x, w.shape)
     if with_bias or db is not None:
         db = _shaped(db, "db", x, (F,))
-    n = ctypes.c_int64()
-    with torch.cuda.device(x.device) if x.get_device() != torch.cuda.current_device() else nullcontext():
-        _check(lib().hla_linear_workspace(T, K, F, act_code, code, ctypes.byref(n)))
-    work = x.new_empty(n.value, dtype=torch.uint8) if n.value else None
+    work, n = _linear_work(x, T, K, F, act_code, code, 1)
     _call(x, lib().hla_linear_bwd, _ptr(x), _ptr(w), _ptr(pre) if act_code else 0, _ptr(dy), act_code,
-          _ptr(dx), _ptr(dw), _ptr(db), T, K, F, code, _ptr(work), n.value)
+          _ptr(dx), _ptr(dw), _ptr(db), T, K, F, code, _ptr(work), n)
     return dx, dw, db

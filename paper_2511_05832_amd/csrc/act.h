@@ -42,40 +42,61 @@ __device__ __forceinline__ float logistic(float z) {
 // gelu_tanh(z) = z / 2 (1 + tanh u) = z logistic(2 u), u = sqrt(2 / pi) (z + 0.044715 z^3).
 constexpr float kGeluC = 0.79788456080286536f, kGeluA = 0.044715f;
 
+// (beyond 30 the derivative is 0 or 1, and z^2 must not overflow)
 template <bool EXACT>
-__device__ __forceinline__ float act_of(int act, float z) {
-  switch (act) {
-    case HLA_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
-    case HLA_ACT_GELU: {
-      float density;
-      return z * normal_cdf<EXACT>(z, density);
+__device__ __forceinline__ float gelu_tanh_grad(float z) {
+  const float s = logistic<EXACT>(2.f * kGeluC * __builtin_fmaf(kGeluA * z * z, z, z));
+  const float g = __builtin_fmaf(z * s * (1.f - s), 2.f * kGeluC * __builtin_fmaf(3.f * kGeluA * z, z, 1.f), s);
+  return fabsf(z) > 30.f ? (z > 0.f ? 1.f : 0.f) : g;
+}
+
+// z[e] = act(z[e]) for N values (one branch for all of them).
+template <bool EXACT, int N>
+__device__ __forceinline__ void apply_act(int act, float (&z)[N]) {
+  float density;
+  if (act == HLA_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] = z[e] > 0.f ? z[e] : (z[e] != z[e] ? z[e] : 0.f);
+  } else if (act == HLA_ACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      if constexpr (EXACT) z[e] *= normal_cdf<true>(z[e], density);
+      else {   // max(z, 0) - |z| Phi(-|z|); beyond 88 the tail is 0 (and inf * 0 must not be formed)
+        const float a = fminf(fabsf(z[e]), 88.f);
+        z[e] = __builtin_fmaf(-a, normal_tail(a, density), z[e] < 0.f ? 0.f : z[e]);
+      }
     }
-    case HLA_ACT_GELU_TANH: return z * logistic<EXACT>(2.f * kGeluC * __builtin_fmaf(kGeluA * z * z, z, z));
-    case HLA_ACT_SILU: return z * logistic<EXACT>(z);
-    default: return z;
+  } else if (act == HLA_ACT_GELU_TANH) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] *= logistic<EXACT>(2.f * kGeluC * __builtin_fmaf(kGeluA * z[e] * z[e], z[e], z[e]));
+  } else if (act == HLA_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] *= logistic<EXACT>(z[e]);
   }
 }
 
-template <bool EXACT>
-__device__ __forceinline__ float act_grad(int act, float z) {
-  switch (act) {
-    case HLA_ACT_RELU: return z > 0.f ? 1.f : 0.f;
-    case HLA_ACT_GELU: {
+// z[e] = act'(z[e])
+template <bool EXACT, int N>
+__device__ __forceinline__ void apply_grad(int act, float (&z)[N]) {
+  if (act == HLA_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] = z[e] > 0.f ? 1.f : 0.f;
+  } else if (act == HLA_ACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
       float density;
-      const float cdf = normal_cdf<EXACT>(z, density);
-      return __builtin_fmaf(z, density, cdf);
+      const float cdf = normal_cdf<EXACT>(z[e], density);
+      z[e] = __builtin_fmaf(z[e], density, cdf);
     }
-    case HLA_ACT_GELU_TANH: {
-      // (beyond 30 the derivative is 0 or 1, and z^2 must not overflow)
-      if (fabsf(z) > 30.f) return z > 0.f ? 1.f : 0.f;
-      const float s = logistic<EXACT>(2.f * kGeluC * __builtin_fmaf(kGeluA * z * z, z, z));
-      return __builtin_fmaf(z * s * (1.f - s), 2.f * kGeluC * __builtin_fmaf(3.f * kGeluA * z, z, 1.f), s);
+  } else if (act == HLA_ACT_GELU_TANH) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] = gelu_tanh_grad<EXACT>(z[e]);
+  } else if (act == HLA_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float s = logistic<EXACT>(z[e]);
+      z[e] = s * __builtin_fmaf(z[e], 1.f - s, 1.f);
     }
-    case HLA_ACT_SILU: {
-      const float s = logistic<EXACT>(z);
-      return s * __builtin_fmaf(z, 1.f - s, 1.f);
-    }
-    default: return 1.f;
   }
 }
 

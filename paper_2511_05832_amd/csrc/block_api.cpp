@@ -391,7 +391,7 @@ extern "C" {
 
 hla_status hla_linear(const void *x, const void *w, const void *bias, const void *residual,
                       hla_act act, void *y, void *pre, int64_t T, int64_t K, int64_t F,
-                      hla_dtype dtype, hla_stream_t stream) {
+                      hla_dtype dtype, void *work, int64_t work_bytes, hla_stream_t stream) {
   LinearArgs a;
   hla_status st = linear_sizes(T, K, F, act, dtype, &a);
   if (st != HLA_OK) return st;
@@ -400,8 +400,12 @@ hla_status hla_linear(const void *x, const void *w, const void *bias, const void
   // (residual == y is allowed: each element is read before it is written, by one thread)
   const Tensor in[4] = {{"x", x, T * K * es}, {"w", w, F * K * es}, {"bias", bias, F * es},
                         {"residual", residual == y ? nullptr : residual, T * F * es}};
-  const Tensor out[2] = {{"y", y, T * F * es}, {"pre", pre, T * F * es}};
-  if ((st = linear_tensors(in, 4, out, 2)) != HLA_OK) return st;
+  a.parts = true;
+  const int64_t need = linear_fwd_work(a, dtype);
+  a.parts = need > 0 && work && work_bytes >= need;
+  const Tensor out[3] = {{"y", y, T * F * es}, {"pre", pre, T * F * es}, {"work", a.parts ? work : nullptr, need}};
+  if ((st = linear_tensors(in, 4, out, 3)) != HLA_OK) return st;
+  a.work = work;
   a.x = x;
   a.w = w;
   a.bias = bias;
@@ -412,13 +416,14 @@ hla_status hla_linear(const void *x, const void *w, const void *bias, const void
 }
 
 hla_status hla_linear_workspace(int64_t T, int64_t K, int64_t F, hla_act act, hla_dtype dtype,
-                                int64_t *bytes) {
+                                int32_t backward, int64_t *bytes) {
   LinearArgs a;
   if (!bytes) return fail(HLA_ERR_INVALID_ARG, "bytes is NULL");
   hla_status st = linear_sizes(T, K, F, act, dtype, &a);
   if (st != HLA_OK) return st;
   a.dx = a.dw = a.db = bytes;   // (all of them; the addresses are not used)
-  *bytes = linear_work(a, (int)dtype_size(dtype)).bytes;
+  a.parts = true;
+  *bytes = backward ? linear_bwd_work(a, dtype).bytes : linear_fwd_work(a, dtype);
   return HLA_OK;
 }
 
@@ -442,7 +447,7 @@ hla_status hla_linear_bwd(const void *x, const void *w, const void *pre, const v
   a.dx = dx;
   a.dw = dw;
   a.db = db;
-  const int64_t es = dtype_size(dtype), need = linear_work(a, (int)es).bytes;
+  const int64_t es = dtype_size(dtype), need = linear_bwd_work(a, dtype).bytes;
   const Tensor in[4] = {{"x", x, T * K * es}, {"w", w, F * K * es}, {"pre", pre, T * F * es}, {"dy", dy, T * F * es}};
   const Tensor out[4] = {{"dx", dx, T * K * es}, {"dw", dw, F * K * es}, {"db", db, F * es},
                          {"work", need ? work : nullptr, need}};

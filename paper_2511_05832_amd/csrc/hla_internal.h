@@ -215,18 +215,20 @@ int cross_bwd_splits(const CrossArgs &a);
 hipError_t launch_cross_fwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s);
 hipError_t launch_cross_bwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s);
 
-// The linear layer (forward: x, w, bias, residual, y, pre; backward: x, w, pre, dy, dx,
-// dw, db, work).
+// The linear layer (forward: x, w, bias, residual, y, pre, work; backward: x, w, pre, dy,
+// dx, dw, db, work).
 struct LinearArgs {
   const void *x, *w, *bias, *residual, *dy;
   void *y, *pre, *dx, *dw, *db, *work;
   int32_t T, K, F, act;
+  bool parts;   // forward: the contraction may be split (work holds the partial sums)
 };
 // Byte offsets of the backward's workspace, and its size.
 struct LinearWork {
   int64_t dz, part, sums, bytes;
 };
-LinearWork linear_work(const LinearArgs &a, int elem_size);
+LinearWork linear_bwd_work(const LinearArgs &a, hla_dtype dtype);
+int64_t linear_fwd_work(const LinearArgs &a, hla_dtype dtype);
 hipError_t launch_linear(const LinearArgs &a, hla_dtype dtype, hipStream_t s);
 hipError_t launch_linear_bwd(const LinearArgs &a, hla_dtype dtype, hipStream_t s);
 

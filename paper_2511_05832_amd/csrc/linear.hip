@@ -34,21 +34,21 @@ template <>
 struct Type<float> {
   static constexpr int V = 4;
   typedef f32x4 Op;
-  // one step of 8 contracted elements (lane half h: elements 16 h + 4 s .. + 3 of the stage)
+  // one step of 8 contracted elements (lane half h: elements KT / 2 h + 4 s .. + 3 of the stage)
   static __device__ __forceinline__ void mma(const Op &a, const Op &b, f32x16 &acc) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], acc, 0, 0, 0);
   }
 };
 
-constexpr int KB = 128;   // bytes of contraction per stage: 64 bf16 or 32 fp32 elements, four steps
-
-// One operand's tile of R rows (or columns) by a stage of the contraction, in LDS.
-//  TR = false: R rows of KB bytes, 16-byte chunk c at c ^ (row % 8).
+// One operand's tile of R rows (or columns) by a stage of the contraction, in LDS: KB
+// bytes of it per row, KB / 32 steps.
+//  TR = false: R rows of KB bytes, 16-byte chunk c at c ^ (row % 8) (KB = 128) or c ^
+//  (row / 2 % 4) (KB = 64), which puts the rows of a read on separate banks.
 //  TR = true: the stage's elements as rows of R values, as in memory; bf16: chunk c of
 //  row r at c ^ (2 (r % 4) + r / 8 % 2), which keeps the transposing reads (four rows
 //  by two chunks) on separate banks; fp32 is read a value per lane, rows as they are.
-template <typename T, int R, bool TR, int NT>
+template <typename T, int R, bool TR, int NT, int KB>
 struct Operand {
   static constexpr int V = Type<T>::V, KT = KB / (int)sizeof(T), BYTES = R * KB;
   static constexpr int COPIES = BYTES / 16 / NT;      // per thread and stage
@@ -59,7 +59,7 @@ struct Operand {
   int64_t step;           // bytes per stage
 
   static __device__ __forceinline__ int swz(int row) {
-    if (!TR) return row & 7;
+    if (!TR) return KB == 128 ? row & 7 : (row >> 1) & 3;
     return sizeof(T) == 2 ? (2 * (row & 3)) | ((row >> 3) & 1) : 0;
   }
   // Rows (columns) from r0 on of a matrix with n of them, ld elements between memory
@@ -92,14 +92,16 @@ struct Operand {
 };
 
 // LDS offsets of a wave's NBLK blocks of 32 rows from row `first` of a tile on.
-template <typename T, int R, bool TR, int NBLK>
+template <typename T, int R, bool TR, int NBLK, int KB>
 struct Reader {
   using Op = typename Type<T>::Op;
+  static constexpr int KT = KB / (int)sizeof(T);
   int at[NBLK], sw;
   __device__ __forceinline__ void init(int first, int lane) {
     const int col = lane & 31, half = lane >> 5;
     if constexpr (!TR) {
-      sw = sizeof(T) == 2 ? (half ^ (col & 7)) * 16 : ((4 * half) ^ (col & 7)) * 16;
+      const int x = KB == 128 ? col & 7 : (col >> 1) & 3;
+      sw = ((sizeof(T) == 2 ? half : KB / 32 * half) ^ x) * 16;
 #pragma unroll
       for (int b = 0; b < NBLK; ++b) at[b] = (first + 32 * b + col) * KB;
     } else if constexpr (sizeof(T) == 2) {
@@ -111,10 +113,10 @@ struct Reader {
       }
     } else {
 #pragma unroll
-      for (int b = 0; b < NBLK; ++b) at[b] = 16 * half * R * 4 + (first + 32 * b + col) * 4;
+      for (int b = 0; b < NBLK; ++b) at[b] = KT / 2 * half * R * 4 + (first + 32 * b + col) * 4;
     }
   }
-  // this lane's operand of block b at step s (0 .. 3)
+  // this lane's operand of block b at step s
   __device__ __forceinline__ Op read(const char *tile, int b, int s) const {
     if constexpr (!TR) {
       return *reinterpret_cast<const Op *>(tile + at[b] + (sw ^ (sizeof(T) == 2 ? s * 32 : s * 16)));
@@ -129,6 +131,8 @@ struct Reader {
   }
 };
 
+constexpr int kGroup = 4;   // tiles along NA that are walked together
+
 enum Epilogue { EPI_LAYER = 0, EPI_PLAIN = 1, EPI_PART = 2 };
 
 struct GemmArgs {
@@ -140,58 +144,72 @@ struct GemmArgs {
   void *out, *pre;
   float *part;               // [splits, NB, NA]
   int32_t act;
-  FastDiv adiv, tdiv;        // division by the tiles along NA, and by all tiles of a split
+  int32_t na;                // tiles along NA
+  FastDiv gdiv, tdiv;        // division by the tiles of a group, and by all tiles of a split
 };
 
 // V consecutive results of the layer from z before its bias (fp32) on.
 template <typename T>
-__device__ __forceinline__ void finish(const GemmArgs &p, float (&z)[Type<T>::V], int64_t row, int f) {
+using Vec = T __attribute__((ext_vector_type(Type<T>::V)));
+// A result's chunk past the caches (16384 x 4096 results with their z and a residual 194
+// -> 182 us).
+template <typename T>
+__device__ __forceinline__ void store_through(T *p, const Vec<T> &v) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4 *>(p));
+}
+template <typename T>
+__device__ __forceinline__ Vec<T> bias_of(const GemmArgs &p, int f) {
+  return p.bias ? *reinterpret_cast<const Vec<T> *>(static_cast<const T *>(p.bias) + f) : Vec<T>{};
+}
+template <typename T>
+__device__ __forceinline__ void finish(const GemmArgs &p, float (&z)[Type<T>::V], const Vec<T> &bias,
+                                       const Vec<T> &residual, int64_t row, int f) {
   constexpr int V = Type<T>::V;
-  typedef T vec __attribute__((ext_vector_type(V)));
+  typedef Vec<T> vec;
   const int64_t at = row * p.NA + f;
-  if (p.bias) {
-    const vec b = *reinterpret_cast<const vec *>(static_cast<const T *>(p.bias) + f);
 #pragma unroll
-    for (int e = 0; e < V; ++e) z[e] += (float)b[e];
-  }
+  for (int e = 0; e < V; ++e) z[e] += (float)bias[e];
   vec o;
   if (p.pre) {
 #pragma unroll
     for (int e = 0; e < V; ++e) o[e] = (T)z[e];
-    *reinterpret_cast<vec *>(static_cast<T *>(p.pre) + at) = o;
+    store_through(static_cast<T *>(p.pre) + at, o);
   }
-  if (p.act != HLA_ACT_NONE) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) z[e] = act_of<sizeof(T) == 4>(p.act, z[e]);
-  }
+  apply_act<sizeof(T) == 4>(p.act, z);
   if (p.residual) {
-    const vec r = *reinterpret_cast<const vec *>(static_cast<const T *>(p.residual) + at);
 #pragma unroll
-    for (int e = 0; e < V; ++e) z[e] += (float)r[e];
+    for (int e = 0; e < V; ++e) z[e] += (float)residual[e];
   }
 #pragma unroll
   for (int e = 0; e < V; ++e) o[e] = (T)z[e];
-  *reinterpret_cast<vec *>(static_cast<T *>(p.out) + at) = o;
+  store_through(static_cast<T *>(p.out) + at, o);
 }
 
-// Output tiles of TB rows by TA columns by WA x WB waves, a ring of two stages.
-template <typename T, int TA, int TB, int WA, int WB, bool AT, bool BT, int EPI>
-__global__ void __launch_bounds__(64 * WA * WB, TA * TB > 128 * 128 ? 2 : 2) gemm_kernel(GemmArgs p) {
+// Output tiles of TB rows by TA columns by WA x WB waves, a ring of RING stages of KB
+// bytes of every row.
+template <typename T, int TA, int TB, int WA, int WB, int KB, int RING, bool AT, bool BT, int EPI>
+__global__ void __launch_bounds__(64 * WA * WB, 2) gemm_kernel(GemmArgs p) {
   constexpr int NT = 64 * WA * WB, V = Type<T>::V, KT = KB / (int)sizeof(T);
   constexpr int AB = TA / WA / 32, BB = TB / WB / 32;
-  using OA = Operand<T, TA, AT, NT>;
-  using OB = Operand<T, TB, BT, NT>;
+  using OA = Operand<T, TA, AT, NT, KB>;
+  using OB = Operand<T, TB, BT, NT, KB>;
+  constexpr int LPT = OA::COPIES + OB::COPIES;
+  static_assert(LPT * (RING - 2) < 64, "vmcnt range");
   constexpr int STAGE = OA::BYTES + OB::BYTES;
   constexpr int PITCH = TA + 4;                       // floats of a staged output row
-  static_assert(WB * 32 * PITCH * 4 <= 2 * STAGE, "the staged rows must fit the ring");
-  __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
+  static_assert(WB * 32 * PITCH * 4 <= RING * STAGE, "the staged rows must fit the ring");
+  __shared__ __attribute__((aligned(16))) char lds[RING * STAGE];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int wa = wave % WA, wb = wave / WA;
   const int logical = xcd_remap(blockIdx.x, gridDim.x);
   const int sp = (int)fdiv((uint32_t)logical, p.tdiv), tile = logical - sp * (int)p.tdiv.div;
-  const int tb = (int)fdiv((uint32_t)tile, p.adiv), ta = tile - tb * (int)p.adiv.div;
+  // Columns of kGroup tiles, row by row: the workgroups that run at once on an XCD share
+  // few slices of either operand, and the group's A tiles stay in its L2.
+  const int grp = (int)fdiv((uint32_t)tile, p.gdiv), in = tile - grp * (int)p.gdiv.div;
+  const int wide = min(kGroup, p.na - grp * kGroup);
+  const int tb = wide == kGroup ? in / kGroup : in / wide, ta = grp * kGroup + in - tb * wide;
   const int a0 = ta * TA, b0 = tb * TB;
   const int s0 = sp * p.stages, ns = min(p.stages, (p.KC + KT - 1) / KT - s0);
 
@@ -200,13 +218,13 @@ __global__ void __launch_bounds__(64 * WA * WB, TA * TB > 128 * 128 ? 2 : 2) gem
   oa.init(static_cast<const T *>(p.a), p.lda, a0, p.NA, wave, lane);
   ob.init(static_cast<const T *>(p.b), p.ldb, b0, p.NB, wave, lane);
   auto issue = [&](int i) {
-    char *dst = lds + (i & 1) * STAGE;
+    char *dst = lds + (i % RING) * STAGE;
     const int left = p.KC - (s0 + i) * KT;
     oa.issue(s0 + i, left, dst, wave, lane);
     ob.issue(s0 + i, left, dst + OA::BYTES, wave, lane);
   };
-  Reader<T, TA, AT, AB> ra;
-  Reader<T, TB, BT, BB> rb;
+  Reader<T, TA, AT, AB, KB> ra;
+  Reader<T, TB, BT, BB, KB> rb;
   ra.init(wa * 32 * AB, lane);
   rb.init(wb * 32 * BB, lane);
   f32x16 acc[AB][BB];
@@ -215,13 +233,16 @@ __global__ void __launch_bounds__(64 * WA * WB, TA * TB > 128 * 128 ? 2 : 2) gem
 #pragma unroll
     for (int y = 0; y < BB; ++y) acc[x][y] = f32x16{};
 
-  if (ns > 0) issue(0);
-  for (int i = 0; i < ns; ++i) {
-    wait_then_barrier<0>();   // stage i has landed, and every wave is done with stage i - 1
-    if (i + 1 < ns) issue(i + 1);
-    const char *st = lds + (i & 1) * STAGE;
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
+  for (int i = 0; i < RING - 1; ++i)
+    if (i < ns) issue(i);
+  for (int i = 0; i < ns; ++i) {
+    // stage i has landed, and every wave is done with stage i - 1
+    wait_tiles_then_barrier<LPT, RING - 2>(min(RING - 2, ns - 1 - i));
+    if (i + RING - 1 < ns) issue(i + RING - 1);
+    const char *st = lds + (i % RING) * STAGE;
+#pragma unroll
+    for (int s = 0; s < KB / 32; ++s) {
       typename Type<T>::Op xa[AB], xb[BB];
 #pragma unroll
       for (int x = 0; x < AB; ++x) xa[x] = ra.read(st, x, s);
@@ -236,27 +257,44 @@ __global__ void __launch_bounds__(64 * WA * WB, TA * TB > 128 * 128 ? 2 : 2) gem
 
   // Through LDS as fp32 rows, WB * 32 output rows at a time, so that the layer's
   // epilogue rounds once and memory is met in whole rows. Lane (col, half) of block
-  // (x, y) holds row 32 y + col, slots 4g .. 4g + 3 columns 8g + 4 half ..
+  // (x, y) holds row 32 y + col, slots 4g .. 4g + 3 columns 8g + 4 half .. The barriers
+  // wait for LDS only: the stores of one pass drain under the next, and under the next
+  // workgroup's first stages.
   float *stage = reinterpret_cast<float *>(lds);
+  constexpr int W = EPI == EPI_PART ? 4 : V;       // values per lane and store
+  constexpr int CPR = TA / W, ROWS = WB * 32, IT = ROWS * CPR / NT;
+  static_assert(ROWS * CPR % NT == 0 && NT % CPR == 0, "stores must split evenly, a lane's all in one column chunk");
+  const int c = (int)threadIdx.x % CPR, f = a0 + c * W;
+  // (row of this lane's store j of pass y)
+  auto row_at = [&](int y, int j) {
+    const int r = (j * NT + (int)threadIdx.x) / CPR;
+    return b0 + (r >> 5) * 32 * BB + 32 * y + (r & 31);
+  };
+  Vec<T> bias = {}, res[IT] = {};
+  if (EPI == EPI_LAYER && f < p.NA) bias = bias_of<T>(p, f);
 #pragma unroll
   for (int y = 0; y < BB; ++y) {
-    wait_then_barrier<0>();
+    if constexpr (EPI == EPI_LAYER) {   // the residual's rows, in flight while the pass is staged
+      if (p.residual) {
+#pragma unroll
+        for (int j = 0; j < IT; ++j)
+          if (row_at(y, j) < p.NB && f < p.NA)
+            res[j] = *reinterpret_cast<const Vec<T> *>(static_cast<const T *>(p.residual) + (int64_t)row_at(y, j) * p.NA + f);
+      }
+    }
+    wait_then_barrier<63>();
 #pragma unroll
     for (int x = 0; x < AB; ++x)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *reinterpret_cast<f32x4 *>(stage + (wb * 32 + col) * PITCH + (wa * AB + x) * 32 + 8 * g + 4 * half) =
             f32x4{acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
-    wait_then_barrier<0>();
-    constexpr int W = EPI == EPI_PART ? 4 : V;       // values per lane and store
-    constexpr int CPR = TA / W, ROWS = WB * 32;
-    static_assert(ROWS * CPR % NT == 0, "stores must split evenly");
-#pragma unroll 2
-    for (int j = 0; j < ROWS * CPR / NT; ++j) {
-      const int q = j * NT + (int)threadIdx.x, r = q / CPR, c = q % CPR;
-      const int row = b0 + (r >> 5) * 32 * BB + 32 * y + (r & 31), f = a0 + c * W;
+    wait_then_barrier<63>();
+#pragma unroll
+    for (int j = 0; j < IT; ++j) {
+      const int row = row_at(y, j);
       if (row >= p.NB || f >= p.NA) continue;
-      const float *src = stage + r * PITCH + c * W;
+      const float *src = stage + (j * NT + (int)threadIdx.x) / CPR * PITCH + c * W;
       if constexpr (EPI == EPI_PART) {
         *reinterpret_cast<f32x4 *>(p.part + ((int64_t)sp * p.NB + row) * p.NA + f) = *reinterpret_cast<const f32x4 *>(src);
       } else {
@@ -264,13 +302,12 @@ __global__ void __launch_bounds__(64 * WA * WB, TA * TB > 128 * 128 ? 2 : 2) gem
 #pragma unroll
         for (int e = 0; e < V; e += 4) *reinterpret_cast<f32x4 *>(z + e) = *reinterpret_cast<const f32x4 *>(src + e);
         if constexpr (EPI == EPI_LAYER) {
-          finish<T>(p, z, row, f);
+          finish<T>(p, z, bias, res[j], row, f);
         } else {
-          typedef T vec __attribute__((ext_vector_type(V)));
-          vec o;
+          Vec<T> o;
 #pragma unroll
           for (int e = 0; e < V; ++e) o[e] = (T)z[e];
-          *reinterpret_cast<vec *>(static_cast<T *>(p.out) + (int64_t)row * p.NA + f) = o;
+          store_through(static_cast<T *>(p.out) + (int64_t)row * p.NA + f, o);
         }
       }
     }
@@ -299,7 +336,7 @@ struct Few<float> {
 
 template <typename T, int NB, int NW>
 __global__ void __launch_bounds__(64 * NW) few_kernel(GemmArgs p) {
-  constexpr int V = Type<T>::V, RUN = KB / (int)sizeof(T), UNROLL = NB == 1 ? 4 : 2;
+  constexpr int V = Type<T>::V, RUN = 128 / (int)sizeof(T), UNROLL = NB == 1 ? 4 : 2;
   typedef typename Type<T>::Op Op;
   __shared__ __attribute__((aligned(16))) f32x4 sums[NW][NB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -361,7 +398,9 @@ __global__ void __launch_bounds__(64 * NW) few_kernel(GemmArgs p) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) z[e + j] = s[j];
     }
-    finish<T>(p, z, t, f);
+    Vec<T> r = {};
+    if (p.residual) r = *reinterpret_cast<const Vec<T> *>(static_cast<const T *>(p.residual) + (int64_t)t * p.NA + f);
+    finish<T>(p, z, bias_of<T>(p, f), r, t, f);
   }
 }
 
@@ -384,9 +423,13 @@ __global__ void __launch_bounds__(256) dz_kernel(const T *dy, const T *pre, T *d
       vec g = *reinterpret_cast<const vec *>(dy + at);
       if (dz) {
         const vec z = *reinterpret_cast<const vec *>(pre + at);
+        float slope[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) slope[e] = (float)z[e];
+        apply_grad<sizeof(T) == 4>(act, slope);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const float d = (float)g[e] * act_grad<sizeof(T) == 4>(act, (float)z[e]);
+          const float d = (float)g[e] * slope[e];
           s[e] += d;
           g[e] = (T)d;
         }
@@ -428,42 +471,92 @@ __global__ void __launch_bounds__(256) sum_kernel(const float *part, T *out, int
   }
 }
 
+// The layer's epilogue over partial sums of its products: V columns of a row per thread.
+template <typename T>
+__global__ void __launch_bounds__(256) finish_kernel(GemmArgs p, int n) {
+  constexpr int V = Type<T>::V;
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V, len = (int64_t)p.NB * p.NA;
+  if (i >= len) return;
+  const int64_t row = i / p.NA;
+  const int f = (int)(i - row * p.NA);
+  float z[V] = {};
+  for (int k = 0; k < n; ++k)
+#pragma unroll
+    for (int e = 0; e < V; e += 4) {
+      const f32x4 x = *reinterpret_cast<const f32x4 *>(p.part + k * len + i + e);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) z[e + j] += x[j];
+    }
+  Vec<T> r = {};
+  if (p.residual) r = *reinterpret_cast<const Vec<T> *>(static_cast<const T *>(p.residual) + i);
+  finish<T>(p, z, bias_of<T>(p, f), r, row, f);
+}
+
 // ---------------------------------------------------------------------------
 // Which tile, and into how many parts the contraction is split.
+//  fp32: 64 x 64, 128 bytes by 2 stages (32 KiB). The matrix cores are slow enough here
+//    that small tiles keep them busy, and even out (4096 tokens, 1024 -> 1024: 75 us, 128 x
+//    128 79; 192 -> 768: 19 against 30).
+//  bf16: 256 x 256 (128 KiB, one workgroup per CU) where such tiles fill the CUs and the
+//    contraction is long enough to pay for a tile's first stage and its stores: 16384 x
+//    1024 by 4096 contracted 112 us against 131 with 128 x 128; but 65536 x 768 by 192:
+//    54 against 47. Or, where parts are allowed, a quarter of the CUs and over 2048
+//    contracted elements for each part (4096 x 1024 by 16384 in four parts 125 us, 128 x
+//    128 in two 128).
+//    128 x 128 where those are at least three to two CUs, or, in parts, 8 stages for
+//    every workgroup (768 x 192 by 65536: 32 us, 64 x 64 37); two workgroups per CU with
+//    2 stages of 128 bytes, or three with 3 stages of 64 for a layer of a short
+//    contraction (65536 tokens, 192 -> 768: 47 us against 50).
+//    64 x 64 by 4 stages otherwise (2048 tokens, 1024 -> 1024: 11 us, 128 x 128 16).
+// Parts: as many as fill the CUs' workgroups, of at least four stages each.
 struct Plan {
-  int tile;       // 256, 128 or 64 a side
+  int tile, kb;   // tile side, bytes of contraction per stage
   int splits;
   int stages;     // per split
 };
 
-Plan plan_of(int64_t NA, int64_t NB, int64_t KC, int kt, bool splittable) {
+template <typename T>
+Plan plan_of(int64_t NA, int64_t NB, int64_t KC, bool layer, bool parts) {
   const int64_t cus = device_cu_count();
   auto tiles = [&](int t) { return ((NA + t - 1) / t) * ((NB + t - 1) / t); };
-  Plan p;
-  p.tile = tiles(256) >= cus / 2 && kt == 64 ? 256 : (tiles(128) >= cus / 2 || splittable ? 128 : 64);
-  const int64_t stages = (KC + kt - 1) / kt;
-  int64_t splits = 1;
-  if (splittable) splits = std::max<int64_t>(1, std::min(cus / tiles(p.tile), stages / 4));
-  p.stages = (int)((stages + splits - 1) / splits);
-  p.splits = (int)((stages + p.stages - 1) / p.stages);
-  return p;
+  auto make = [&](int tile, int kb, int64_t wgs, int64_t least) {
+    const int64_t stages = (KC + kb / (int64_t)sizeof(T) - 1) / (kb / (int64_t)sizeof(T));
+    const int64_t splits = parts ? std::max<int64_t>(1, std::min(wgs / tiles(tile), stages / least)) : 1;
+    Plan p = {tile, kb, 1, (int)((stages + splits - 1) / splits)};
+    p.splits = (int)((stages + p.stages - 1) / p.stages);
+    return p;
+  };
+  if (sizeof(T) == 4) return make(64, 128, 4 * cus, 4);
+  const int64_t n256 = tiles(256), n128 = tiles(128);
+  const bool fills = n256 * 5 >= (n256 + cus - 1) / cus * cus * 4;   // four fifths of its rounds
+  if (KC >= 512 && fills) return make(256, 128, cus, 4);
+  if (parts && !layer && 4 * n256 >= cus && KC * n256 / cus >= 2048) return make(256, 128, cus, 4);
+  if (2 * n128 >= 3 * cus) return layer && KC < 512 ? make(128, 64, 1, 1) : make(128, 128, 2 * cus, 4);
+  if (parts && !layer && n128 * ((KC + 63) / 64) >= 16 * cus) return make(128, 128, 2 * cus, 4);
+  return make(64, 128, 2 * cus, layer ? 8 : 4);
 }
 
 template <typename T, bool AT, bool BT, int EPI>
 hipError_t launch_gemm(GemmArgs &p, const Plan &plan, hipStream_t s) {
   const int64_t na = (p.NA + plan.tile - 1) / plan.tile, nb = (p.NB + plan.tile - 1) / plan.tile;
   p.stages = plan.stages;
-  p.adiv = make_fastdiv((uint32_t)na);
+  p.na = (int32_t)na;
+  p.gdiv = make_fastdiv((uint32_t)(kGroup * nb));
   p.tdiv = make_fastdiv((uint32_t)(na * nb));
   const dim3 grid((uint32_t)(na * nb * plan.splits));
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 4) {
+    hipLaunchKernelGGL((gemm_kernel<T, 64, 64, 2, 2, 128, 2, AT, BT, EPI>), grid, dim3(256), 0, s, p);
+  } else {
     if (plan.tile == 256) {
-      hipLaunchKernelGGL((gemm_kernel<T, 256, 256, 4, 2, AT, BT, EPI>), grid, dim3(512), 0, s, p);
-      return hipGetLastError();
+      hipLaunchKernelGGL((gemm_kernel<T, 256, 256, 4, 2, 128, 2, AT, BT, EPI>), grid, dim3(512), 0, s, p);
+    } else if (plan.tile == 64) {
+      hipLaunchKernelGGL((gemm_kernel<T, 64, 64, 2, 2, 128, 4, AT, BT, EPI>), grid, dim3(256), 0, s, p);
+    } else if (plan.kb == 128) {
+      hipLaunchKernelGGL((gemm_kernel<T, 128, 128, 2, 2, 128, 2, AT, BT, EPI>), grid, dim3(256), 0, s, p);
+    } else if constexpr (EPI == EPI_LAYER) {
+      hipLaunchKernelGGL((gemm_kernel<T, 128, 128, 2, 2, 64, 3, AT, BT, EPI>), grid, dim3(256), 0, s, p);
     }
   }
-  if (plan.tile == 128) hipLaunchKernelGGL((gemm_kernel<T, 128, 128, 2, 2, AT, BT, EPI>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((gemm_kernel<T, 64, 64, 2, 2, AT, BT, EPI>), grid, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
@@ -479,6 +572,11 @@ hipError_t product(GemmArgs &p, const Plan &plan, hipStream_t s) {
   return hipGetLastError();
 }
 
+constexpr int kFewTokens = 64;
+
+template <typename T>
+Plan layer_plan(const LinearArgs &a) { return plan_of<T>(a.F, a.T, a.K, true, a.parts); }
+
 template <typename T>
 hipError_t fwd(const LinearArgs &a, hipStream_t s) {
   GemmArgs p = {};
@@ -493,7 +591,7 @@ hipError_t fwd(const LinearArgs &a, hipStream_t s) {
   p.out = a.y;
   p.pre = a.pre;
   p.act = a.act;
-  if (a.T <= 64) {
+  if (a.T <= kFewTokens) {
     const dim3 grid((uint32_t)((a.F + 15) / 16));
     // (more waves to a workgroup where there are few workgroups)
     const bool wide = (int)grid.x >= device_cu_count();
@@ -506,7 +604,14 @@ hipError_t fwd(const LinearArgs &a, hipStream_t s) {
     }
     return hipGetLastError();
   }
-  return launch_gemm<T, false, false, EPI_LAYER>(p, plan_of(a.F, a.T, a.K, KB / (int)sizeof(T), false), s);
+  const Plan plan = layer_plan<T>(a);
+  if (plan.splits == 1) return launch_gemm<T, false, false, EPI_LAYER>(p, plan, s);
+  p.part = static_cast<float *>(a.work);
+  hipError_t e = launch_gemm<T, false, false, EPI_PART>(p, plan, s);
+  if (e != hipSuccess) return e;
+  const int64_t n = (int64_t)a.T * a.F / Type<T>::V;
+  hipLaunchKernelGGL((finish_kernel<T>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, s, p, plan.splits);
+  return hipGetLastError();
 }
 
 // Runs of rows of the dz launch: workgroups for every CU four times over.
@@ -518,8 +623,8 @@ int dz_rows(const LinearArgs &a, int V) {
 
 template <typename T>
 hipError_t bwd(const LinearArgs &a, hipStream_t s) {
-  constexpr int V = Type<T>::V, KT = KB / (int)sizeof(T);
-  const LinearWork w = linear_work(a, (int)sizeof(T));
+  constexpr int V = Type<T>::V;
+  const LinearWork w = linear_bwd_work(a, sizeof(T) == 2 ? HLA_BF16 : HLA_F32);
   char *work = static_cast<char *>(a.work);
   T *dz = reinterpret_cast<T *>(work + w.dz);
   float *part = reinterpret_cast<float *>(work + w.part), *sums = reinterpret_cast<float *>(work + w.sums);
@@ -549,7 +654,7 @@ hipError_t bwd(const LinearArgs &a, hipStream_t s) {
     p.KC = a.F;
     p.out = a.dx;
     p.part = part;
-    if ((e = product<T, true, false>(p, plan_of(a.K, a.T, a.F, KT, true), s)) != hipSuccess) return e;
+    if ((e = product<T, true, false>(p, plan_of<T>(a.K, a.T, a.F, false, true), s)) != hipSuccess) return e;
   }
   if (a.dw) {
     GemmArgs p = {};
@@ -562,28 +667,47 @@ hipError_t bwd(const LinearArgs &a, hipStream_t s) {
     p.KC = a.T;
     p.out = a.dw;
     p.part = part;
-    if ((e = product<T, true, true>(p, plan_of(a.K, a.F, a.T, KT, true), s)) != hipSuccess) return e;
+    if ((e = product<T, true, true>(p, plan_of<T>(a.K, a.F, a.T, false, true), s)) != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
 }  // namespace
 
-// Workspace of the backward: dz, the products' partial sums (dx's and dW's in turn),
-// the bias' partial sums.
-LinearWork linear_work(const LinearArgs &a, int es) {
-  const int V = 16 / es, kt = KB / es;
+namespace {
+
+template <typename T>
+LinearWork work_of(const LinearArgs &a) {
   auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
   auto parts = [&](const Plan &p, int64_t len) { return p.splits == 1 ? 0 : (int64_t)p.splits * len * 4; };
   LinearWork w;
   w.dz = 0;
-  w.part = a.act != HLA_ACT_NONE ? up((int64_t)a.T * a.F * es) : 0;
-  const int64_t dx = a.dx ? parts(plan_of(a.K, a.T, a.F, kt, true), (int64_t)a.T * a.K) : 0;
-  const int64_t dw = a.dw ? parts(plan_of(a.K, a.F, a.T, kt, true), (int64_t)a.F * a.K) : 0;
+  w.part = a.act != HLA_ACT_NONE ? up((int64_t)a.T * a.F * sizeof(T)) : 0;
+  const int64_t dx = a.dx ? parts(plan_of<T>(a.K, a.T, a.F, false, true), (int64_t)a.T * a.K) : 0;
+  const int64_t dw = a.dw ? parts(plan_of<T>(a.K, a.F, a.T, false, true), (int64_t)a.F * a.K) : 0;
   w.sums = w.part + up(std::max(dx, dw));
-  const int rows = dz_rows(a, V);
+  const int rows = dz_rows(a, Type<T>::V);
   w.bytes = w.sums + (a.db ? up((int64_t)((a.T + rows - 1) / rows) * a.F * 4) : 0);
   return w;
+}
+
+template <typename T>
+int64_t layer_work(const LinearArgs &a) {
+  if (a.T <= kFewTokens) return 0;
+  const Plan p = layer_plan<T>(a);
+  return p.splits == 1 ? 0 : (int64_t)p.splits * a.T * a.F * 4;
+}
+
+}  // namespace
+
+// Workspace of the backward: dz, the products' partial sums (dx's and dW's in turn),
+// the bias' partial sums.
+LinearWork linear_bwd_work(const LinearArgs &a, hla_dtype dtype) {
+  return dtype == HLA_BF16 ? work_of<__bf16>(a) : work_of<float>(a);
+}
+// Workspace of the forward where its contraction may be split (a.parts).
+int64_t linear_fwd_work(const LinearArgs &a, hla_dtype dtype) {
+  return dtype == HLA_BF16 ? layer_work<__bf16>(a) : layer_work<float>(a);
 }
 
 hipError_t launch_linear(const LinearArgs &a, hla_dtype dtype, hipStream_t s) {

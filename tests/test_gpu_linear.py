@@ -113,6 +113,26 @@ def test_forward_and_backward(size, act, dtype):
     check_backward(x, w, dy, pre, act, dx, dw, db)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("size", [(70, 4096, 136), (200, 2056, 520), (513, 1032, 64)], ids=str)
+def test_split_contraction_and_without_a_workspace(size, dtype):
+    T, K, F = size
+    x, w, b, r, _ = make(T, K, F, dtype, seed=7)
+    n = ctypes.c_int64()
+    assert hla.lib().hla_linear_workspace(T, K, F, 2, hla._dtype_code(x), 0, ctypes.byref(n)) == hla.HLA_OK
+    assert n.value > 0
+    y, pre = hla.linear(x, w, b, act="gelu", residual=r, with_pre=True)
+    check_forward(x, w, b, r, "gelu", y, pre)
+    for work in (0, n.value - 16):
+        buf = torch.empty(max(work, 16), dtype=torch.uint8, device="cuda")
+        y, pre = torch.empty_like(y), torch.empty_like(pre)
+        st = hla.lib().hla_linear(*(t.data_ptr() for t in (x, w, b, r)), 2, y.data_ptr(), pre.data_ptr(), T, K, F,
+                                  hla._dtype_code(x), buf.data_ptr() if work else 0, work, hla._stream(x))
+        assert st == hla.HLA_OK
+        check_forward(x, w, b, r, "gelu", y, pre)
+
+
 # products large enough for the 256-wide tiles, ragged in every direction
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,size", [(BF, (4200, 328, 3000)), (BF, (3000, 2600, 520)), (F32, (2000, 196, 1300)),
@@ -134,7 +154,7 @@ def test_some_gradients_only(dtype):
     full = hla.linear_bwd(x, w, dy, pre, act="silu", with_bias=True)
     n = ctypes.c_int64()
     code = hla._dtype_code(x)
-    assert hla.lib().hla_linear_workspace(T, K, F, 4, code, ctypes.byref(n)) == hla.HLA_OK
+    assert hla.lib().hla_linear_workspace(T, K, F, 4, code, 1, ctypes.byref(n)) == hla.HLA_OK
     for keep in ((0,), (1,), (2,), (0, 2)):
         outs = [torch.full_like(t, 7.0) for t in full]
         work = torch.empty(max(n.value, 16), dtype=torch.uint8, device="cuda")
@@ -268,9 +288,12 @@ X, W, B, R, Y, P, G, DX, DW, DB, WK = (0x10000000 * i for i in range(1, 12))
     (dict(y=R + 16), INV, "y overlaps residual"),
     (dict(pre=R), INV, "pre overlaps residual"),
     (dict(pre=Y + 64), INV, "pre overlaps y"),
+    (dict(K=4096, work=X, bytes=1 << 24), INV, "work overlaps x"),
+    (dict(K=4096, work=WK + 8, bytes=1 << 24), INV, "aligned"),
 ], ids=str)
 def test_refusals_forward(kw, status, text):
-    a = dict(x=X, w=W, bias=B, residual=R, act=2, y=Y, pre=P, T=128, K=64, F=64, dtype=hla.HLA_BF16)
+    a = dict(x=X, w=W, bias=B, residual=R, act=2, y=Y, pre=P, T=128, K=64, F=64, dtype=hla.HLA_BF16, work=0,
+             bytes=0)
     a.update(kw)
     st = hla.lib().hla_linear(*a.values(), None)
     assert st == status and text in hla.lib().hla_last_error().decode(), hla.lib().hla_last_error()
