@@ -153,9 +153,9 @@ namespace {
 
 CrossStride cross_stride(const ViewShape &s) { return {s.v.batch, s.v.head, s.v.row}; }
 
-// Sizes of a cross attention, into the kernel's arguments.
+// Sizes of a cross attention, into the kernel's arguments, and its workspace.
 hla_status cross_sizes(int64_t B, int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d,
-                       hla_dtype dtype, bool backward, CrossArgs *a) {
+                       hla_dtype dtype, bool backward, CrossArgs *a, int64_t *bytes) {
   if (!dtype_size(dtype)) return fail(HLA_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
   if (B <= 0 || heads <= 0 || kv_heads <= 0 || N <= 0 || M <= 0 || d <= 0)
     return fail(HLA_ERR_INVALID_ARG, "sizes must be positive");
@@ -177,20 +177,14 @@ hla_status cross_sizes(int64_t B, int64_t heads, int64_t kv_heads, int64_t N, in
   a->M = (int32_t)M;
   a->R = (int32_t)R;
   a->Rp = (int32_t)((R + 127) / 128 * 128);
-  a->n_ktiles = (int32_t)((M + 63) / 64);
   a->ndiv = make_fastdiv((uint32_t)N);
-  a->splits = backward ? cross_bwd_splits(*a) : cross_fwd_splits(*a);
+  const bool parts = backward ? cross_bwd_plan(*a) : cross_fwd_plan(*a);
+  *bytes = backward ? 8 * bk * a->Rp + (parts ? bk * a->splits * M * 8 * d : 0)
+                    : (parts ? bk * a->splits * R * (4 * d + 8) : 0);
   return HLA_OK;
 }
 
-int64_t cross_bytes(const CrossArgs &a, int64_t d, bool backward) {
-  const int64_t bk = (int64_t)a.B * a.kv;
-  if (!backward) return a.splits == 1 ? 0 : bk * a.splits * a.R * (4 * d + 8);
-  return 8 * bk * a.Rp + (a.splits == 1 ? 0 : bk * a.splits * a.M * 8 * d);
-}
-
-hla_status cross_work(const CrossArgs &a, int64_t d, bool backward, const void *work, int64_t bytes) {
-  const int64_t need = cross_bytes(a, d, backward);
+hla_status cross_work(int64_t need, const void *work, int64_t bytes) {
   if (!need) return HLA_OK;
   if (!work) return fail(HLA_ERR_INVALID_ARG, "work is NULL, %lld bytes are needed", (long long)need);
   if (!aligned(work, 16)) return fail(HLA_ERR_INVALID_ARG, "work is not 16-byte aligned");
@@ -239,9 +233,7 @@ hla_status hla_cross_attn_workspace(int64_t B, int64_t heads, int64_t kv_heads, 
                                     int64_t *bytes) {
   CrossArgs a;
   if (!bytes) return fail(HLA_ERR_INVALID_ARG, "bytes is NULL");
-  hla_status st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, backward != 0, &a);
-  if (st == HLA_OK) *bytes = cross_bytes(a, d, backward != 0);
-  return st;
+  return cross_sizes(B, heads, kv_heads, N, M, d, dtype, backward != 0, &a, bytes);
 }
 
 hla_status hla_cross_attn_fwd(const hla_view *q, const hla_view *k, const hla_view *v,
@@ -252,17 +244,17 @@ hla_status hla_cross_attn_fwd(const hla_view *q, const hla_view *k, const hla_vi
   hla_status st;
   CrossArgs a = {};
   if (!q || !k || !v || !out) return fail(HLA_ERR_INVALID_ARG, "q, k, v or out is NULL");
-  if ((st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, false, &a)) != HLA_OK) return st;
+  int64_t need = 0;
+  if ((st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, false, &a, &need)) != HLA_OK) return st;
   if ((st = cross_scale(scale, &a)) != HLA_OK) return st;
   if (lse && !aligned(lse, 4)) return fail(HLA_ERR_INVALID_ARG, "lse is not 4-byte aligned");
   if (lengths && !aligned(lengths, 4)) return fail(HLA_ERR_INVALID_ARG, "lengths is not 4-byte aligned");
   const int64_t es = dtype_size(dtype), lse_bytes = lse ? B * heads * N * 4 : 0;
   ViewShape t[4] = {{"q", *q, {B, heads, N}, d, es}, {"k", *k, {B, kv_heads, M}, d, es},
                     {"v", *v, {B, kv_heads, M}, d, es}, {"out", *out, {B, heads, N}, d, es}};
-  const int64_t need = cross_bytes(a, d, false);
   if ((st = cross_views(t, 3, 4, {{"lse", lse, lse_bytes}, {"lengths", lengths, B * 4}, {"work", work, need}})) != HLA_OK)
     return st;
-  if ((st = cross_work(a, d, false, work, work_bytes)) != HLA_OK) return st;
+  if ((st = cross_work(need, work, work_bytes)) != HLA_OK) return st;
   for (int i = 0; i < 3; ++i) {
     if (need && view_clash(t[i], work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps %s", t[i].name);
     if (lse && view_clash(t[i], lse, lse_bytes)) return fail(HLA_ERR_INVALID_ARG, "lse overlaps %s", t[i].name);
@@ -280,7 +272,7 @@ hla_status hla_cross_attn_fwd(const hla_view *q, const hla_view *k, const hla_vi
   a.os = cross_stride(t[3]);
   a.lse = lse;
   a.lengths = lengths;
-  if (a.splits > 1) {
+  if (need) {
     a.part = static_cast<float *>(work);
     a.part_ml = reinterpret_cast<float2 *>(a.part + (int64_t)a.B * a.kv * a.splits * a.R * d);
   }
@@ -296,19 +288,20 @@ hla_status hla_cross_attn_bwd(const hla_view *q, const hla_view *k, const hla_vi
   hla_status st;
   CrossArgs a = {};
   if (!q || !k || !v || !out || !dout || !dq || !dk || !dv) return fail(HLA_ERR_INVALID_ARG, "a tensor is NULL");
-  if ((st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, true, &a)) != HLA_OK) return st;
+  int64_t need = 0;
+  if ((st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, true, &a, &need)) != HLA_OK) return st;
   if ((st = cross_scale(scale, &a)) != HLA_OK) return st;
   if (!lse) return fail(HLA_ERR_INVALID_ARG, "lse is NULL");
   if (!aligned(lse, 4)) return fail(HLA_ERR_INVALID_ARG, "lse is not 4-byte aligned");
   if (lengths && !aligned(lengths, 4)) return fail(HLA_ERR_INVALID_ARG, "lengths is not 4-byte aligned");
-  const int64_t es = dtype_size(dtype), lse_bytes = B * heads * N * 4, need = cross_bytes(a, d, true);
+  const int64_t es = dtype_size(dtype), lse_bytes = B * heads * N * 4;
   ViewShape t[8] = {{"q", *q, {B, heads, N}, d, es},       {"k", *k, {B, kv_heads, M}, d, es},
                     {"v", *v, {B, kv_heads, M}, d, es},    {"out", *out, {B, heads, N}, d, es},
                     {"dout", *dout, {B, heads, N}, d, es}, {"dq", *dq, {B, heads, N}, d, es},
                     {"dk", *dk, {B, kv_heads, M}, d, es},  {"dv", *dv, {B, kv_heads, M}, d, es}};
   if ((st = cross_views(t, 5, 8, {{"lse", lse, lse_bytes}, {"lengths", lengths, B * 4}, {"work", work, need}})) != HLA_OK)
     return st;
-  if ((st = cross_work(a, d, true, work, work_bytes)) != HLA_OK) return st;
+  if ((st = cross_work(need, work, work_bytes)) != HLA_OK) return st;
   for (int i = 0; i < 5; ++i)
     if (view_clash(t[i], work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps %s", t[i].name);
   if (overlaps(lse, lse_bytes, work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps lse");

@@ -55,6 +55,17 @@ __device__ __forceinline__ T *row_ptr(const void *p, const CrossStride &s, int b
   return const_cast<T *>(static_cast<const T *>(p)) + b * s.batch + r.head * s.head + r.n * s.row;
 }
 
+// Workgroup -> piece of work. The pieces are ordered by (batch, key head), whose keys they
+// share, and workgroups go round-robin over the 8 XCDs: runs of `unit` consecutive
+// pieces are dealt to the XCDs in turn, so that a run shares its keys in one L2 while
+// every XCD gets its part of the long and of the short batch elements. (Lengths 4096 and
+// about 2000, 16384 rows each: one contiguous range per XCD leaves half the chip
+// with the long element.) total = pieces; past them the result is >= total.
+__device__ __forceinline__ int deal(int bid, int unit) {
+  const int xcd = bid & 7, slot = bid >> 3, u = slot / unit;
+  return (u * 8 + xcd) * unit + slot - u * unit;
+}
+
 // Keys seen by batch element b.
 __device__ __forceinline__ int keys_of(const CrossArgs &a, int b) {
   return a.lengths ? clampi(sload(a.lengths + b), 0, a.M) : a.M;
@@ -90,164 +101,128 @@ __device__ __forceinline__ void mask_tail(f32x16 &s, int left, int half) {
     s[v] = 16 * (v >> 3) + 8 * half + (v & 7) < left ? s[v] : -__builtin_inff();
 }
 
+// The running softmax of a wave's 32 rows: reference m (log2 units), this lane's half of
+// the sum l about it, O^T about it.
+template <typename T, int D>
+struct Softmax {
+  using Tl = Tile<T, D>;
+  f32x16 o[Tl::NDB];
+  float m, l;
+  bool primed;   // every row of the wave has a finite reference
+  bool fresh;    // no key yet
+
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int db = 0; db < Tl::NDB; ++db) o[db] = f32x16{};
+    m = -__builtin_inff();
+    l = 0.f;
+    primed = false;
+    fresh = true;
+  }
+  // weights of NB blocks in place of their scores; returns the new sum
+  template <int NB>
+  __device__ __forceinline__ float weights(f32x16 (&s)[NB], float scale, float ref) const {
+    float sum[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) sum[b] = b ? 0.f : l;
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        s[b][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][v], scale, -ref));
+        sum[b] += s[b][v];
+      }
+    return NB == 2 ? sum[0] + sum[NB - 1] : sum[0];
+  }
+  // NB blocks of 32 keys at k and v; TAIL: keys from `left` on are not seen. Once all
+  // references are finite the weights are taken against them as they stand, with no
+  // maximum: weights up to 2^32 are harmless in fp32, and as all are >= 0 the new sum
+  // bounds each, so one compare of it (NaN and inf fail it too) accepts them. The first
+  // keys try the reference 0 in the same way, with a lower bound as well. Only where that
+  // fails are the scores formed again and the reference moved, if a score passes it by
+  // more than the slack.
+  template <int NB, bool TAIL>
+  __device__ __forceinline__ void step(const Tl &tl, const char *k, const char *v, const typename Tl::Frag &q,
+                                       float scale, int left, int half) {
+    f32x16 s[NB];
+    auto scores = [&]() {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        tl.rows_times(k + b * 32 * Tl::ROW, q, s[b]);
+        if (TAIL) mask_tail(s[b], left - 32 * b, half);
+      }
+    };
+    scores();
+    float ln = 0.f;
+    bool slow = !primed;
+    if (primed || fresh) {
+      ln = weights(s, scale, fresh ? 0.f : m);
+      const bool bad = !(ln <= 4294967296.f) || (fresh && !(ln >= 1.f / 4294967296.f));
+      slow = false;
+      if (!__ballot(bad)) {
+        if (fresh) m = 0.f;
+        primed = true;
+      } else {
+        slow = true;
+        asm volatile("" ::: "memory");   // (read the keys again rather than keep them in registers)
+        scores();
+      }
+    }
+    if (slow) {
+      float mx = s[0][0];
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[b][e]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale;
+      const bool need = mx > m + kSlack;
+      if (__ballot(need)) {
+        const float m_new = need ? mx : m, alpha = need ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+        l *= alpha;
+#pragma unroll
+        for (int db = 0; db < Tl::NDB; ++db) o[db] *= alpha;
+        m = m_new;
+      }
+      ln = weights(s, scale, m == -__builtin_inff() ? 0.f : m);
+      primed = !__ballot(m == -__builtin_inff());
+    }
+    fresh = false;
+    l = ln;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) tl.cols_times(v + b * 32 * Tl::ROW, s[b], o);
+  }
+  // a tile of 64 keys, `left` of them (and of what follows) seen
+  __device__ __forceinline__ void tile(const Tl &tl, const char *k, const char *v, const typename Tl::Frag &q,
+                                       float scale, int left, int half) {
+    if (left >= BN) {
+      step<2, false>(tl, k, v, q, scale, left, half);
+    } else {
+#pragma unroll 1
+      for (int b = 0; 32 * b < left; ++b)
+        step<1, true>(tl, k + b * 32 * Tl::ROW, v + b * 32 * Tl::ROW, q, scale, left - 32 * b, half);
+    }
+  }
+};
+
 template <typename T, int D>
 constexpr int fwd_ring() { return sizeof(T) == 4 ? 2 : 3; }
 
-template <typename T, int D, int NW>
-__global__ void __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) cross_fwd(CrossArgs a) {
+// Many rows: one workgroup per tile of 128 rows, its four waves on the same key tiles.
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 2) cross_fwd(CrossArgs a) {
   using Tl = Tile<T, D>;
-  constexpr int NDB = Tl::NDB, RING = fwd_ring<T, D>();
+  constexpr int NDB = Tl::NDB, RING = fwd_ring<T, D>(), NW = 4;
   constexpr int STAGE = 2 * BN * Tl::ROW;
   constexpr int AREA = 32 * (Tl::ROW + 16);
   static_assert(NW * AREA <= RING * STAGE, "the rows' staging must fit the ring");
   using Copy = KvCopy<T, D, NW>;
-  static_assert(Copy::LPT * (RING - 2) < 64, "vmcnt range");
+  static_assert(Copy::LPT < 64, "vmcnt range");
   __shared__ __attribute__((aligned(16))) char lds[RING * STAGE];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const int logical = xcd_remap(blockIdx.x, gridDim.x);
-  const int rt = logical % a.n_rtiles, t = logical / a.n_rtiles;
-  const int sp = t % a.splits, bk = t / a.splits, b = bk / a.kv, kvh = bk - b * a.kv;
-
-  // This split's keys [k0, k1): whole tiles but for the last.
-  const int len = keys_of(a, b);
-  const int per = (((len + a.splits - 1) / a.splits) + BN - 1) / BN * BN;
-  const int k0 = min(sp * per, len), k1 = min(k0 + per, len);
-  const int nt = (k1 - k0 + BN - 1) / BN;
-  const char *K = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head);
-  const char *V = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + b * a.vs.batch + kvh * a.vs.head);
-  const uint32_t kr = (uint32_t)a.ks.row * sizeof(T), vr = (uint32_t)a.vs.row * sizeof(T);
-  auto issue = [&](int i) {
-    const int at = k0 + i * BN;
-    Copy::issue(K + (int64_t)at * kr, V + (int64_t)at * vr, kr, vr, k1 - 1 - at, lds + (i % RING) * STAGE, wave, lane);
-  };
-#pragma unroll
-  for (int i = 0; i < RING - 1; ++i)
-    if (i < nt) issue(i);
-
-  // (rows past the last read it and store nothing)
-  const int r0 = (rt * NW + wave) * 32, r = r0 + col;
-  const Row rw = row_of(a, min(r, a.R - 1), kvh);
-  typename Tl::Frag q;
-  Tl::load(q, row_ptr<T>(a.q, a.qs, b, rw), half);
-  Tl tl;
-  tl.init(lane);
-  f32x16 o[NDB];
-#pragma unroll
-  for (int db = 0; db < NDB; ++db) o[db] = f32x16{};
-  float m = -__builtin_inff(), l = 0.f;   // reference (log2 units), this lane's half of the sum
-  wait_vmem_all();
-
-  for (int i = 0; i < nt; ++i) {
-    wait_tiles_then_barrier<Copy::LPT, RING - 2>(min(RING - 2, nt - 1 - i));
-    if (i + RING - 1 < nt) issue(i + RING - 1);
-    const char *st = lds + (i % RING) * STAGE;
-    const int left = k1 - (k0 + i * BN);   // keys of this tile, and beyond
-    // Both blocks of 32 keys together; a last tile of one block leaves the other out.
-    f32x16 s[2];
-    const bool two = left > 32;
-    tl.rows_times(st, q, s[0]);
-    if (two) tl.rows_times(st + 32 * Tl::ROW, q, s[1]);
-    if (left < BN) {
-      if (two) mask_tail(s[1], left - 32, half);
-      else mask_tail(s[0], left, half);
-    }
-    float mx = s[0][0];
-#pragma unroll
-    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[0][v]);
-    if (two) {
-#pragma unroll
-      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[1][v]);
-    }
-    mx = fmaxf(mx, __shfl_xor(mx, 32)) * a.scale_log2;
-    // The reference moves only when the tile's max passes it by the slack (weights
-    // stay <= 2^8; O and l share it).
-    const bool need = mx > m + kSlack;
-    if (__ballot(need)) {
-      const float m_new = need ? mx : m, alpha = need ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
-      l *= alpha;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db) o[db] *= alpha;
-      m = m_new;
-    }
-    const float ref = m == -__builtin_inff() ? 0.f : m;
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      if (kb == 1 && !two) break;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        s[kb][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][v], a.scale_log2, -ref));
-        l += s[kb][v];
-      }
-      tl.cols_times(st + BN * Tl::ROW + kb * 32 * Tl::ROW, s[kb], o);
-    }
-  }
-  l += __shfl_xor(l, 32);
-
-  if (a.splits > 1) {
-    const int64_t at = ((int64_t)bk * a.splits + sp) * a.R + r;
-    if (r < a.R) {
-      float *p = a.part + at * D;
-      Tl::columns(o, half, [&](int c, f32x4 v) { *reinterpret_cast<f32x4 *>(p + c) = v; });
-      if (half == 0) a.part_ml[at] = make_float2(m, l);
-    }
-    return;
-  }
-  wait_then_barrier<0>();   // every wave is done with the ring
-  const int64_t first = ((int64_t)b * a.kv + kvh) * a.R;   // = (b * heads + kvh * G) * N
-  if (a.lse && half == 0 && r < a.R) a.lse[first + r] = lse_of(m, l);
-  const float inv = inv_of(l);
-  // each lane's factor goes into its own row before the rows are staged
-#pragma unroll
-  for (int db = 0; db < NDB; ++db) o[db] *= inv;
-  store_rows<T, D>(lds + wave * AREA, o, 1.f, lane, [&](int i) {
-    return r0 + i < a.R ? row_ptr<T>(a.out, a.os, b, row_of(a, r0 + i, kvh)) : nullptr;
-  });
-}
-
-// Joins the partial sums of the key splits: one thread per row and four columns.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) cross_join(CrossArgs a) {
-  constexpr int TPR = D / 4;
-  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = idx / TPR;
-  if (row >= (int64_t)a.B * a.kv * a.R) return;
-  const int c = (int)(idx % TPR) * 4;
-  const int bk = (int)(row / a.R), r = (int)(row - (int64_t)bk * a.R), b = bk / a.kv, kvh = bk - b * a.kv;
-  const float2 *ml = a.part_ml + (int64_t)bk * a.splits * a.R + r;
-  const float *p = a.part + ((int64_t)bk * a.splits * a.R + r) * D + c;
-  float m = -__builtin_inff();
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[(int64_t)s * a.R].x);
-  const float ref = m == -__builtin_inff() ? 0.f : m;
-  float l = 0.f;
-  f32x4 o = {};
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 e = ml[(int64_t)s * a.R];
-    const f32x4 x = *reinterpret_cast<const f32x4 *>(p + (int64_t)s * a.R * D);
-    const float w = __builtin_amdgcn_exp2f(e.x - ref);
-    l += w * e.y;
-    o += w * x;
-  }
-  if (a.lse && c == 0) a.lse[(int64_t)bk * a.R + r] = lse_of(m, l);
-  put4<T>(row_ptr<T>(a.out, a.os, b, row_of(a, r, kvh)) + c, o * inv_of(l));
-}
-
-// dq, and the rows' statistics for the next kernel: lse log2 e (+inf for a row without
-// a key and for the padding of the last tile, which makes every weight exp2(s - inf) =
-// 0) and -delta.
-template <typename T, int D, int NW>
-__global__ void __launch_bounds__(64 * NW, 2) cross_dq(CrossArgs a) {
-  using Tl = Tile<T, D>;
-  constexpr int NDB = Tl::NDB, RING = fwd_ring<T, D>();
-  constexpr int STAGE = 2 * BN * Tl::ROW;
-  constexpr int AREA = 32 * (Tl::ROW + 16);
-  using Copy = KvCopy<T, D, NW>;
-  __shared__ __attribute__((aligned(16))) char lds[RING * STAGE];
-
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 31, half = lane >> 5;
-  const int logical = xcd_remap(blockIdx.x, gridDim.x);
+  const int logical = deal(blockIdx.x, a.unit);
+  if (logical >= a.total) return;
   const int rt = logical % a.n_rtiles, bk = logical / a.n_rtiles, b = bk / a.kv, kvh = bk - b * a.kv;
   const int len = keys_of(a, b), nt = (len + BN - 1) / BN;
   const char *K = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head);
@@ -261,37 +236,294 @@ __global__ void __launch_bounds__(64 * NW, 2) cross_dq(CrossArgs a) {
   for (int i = 0; i < RING - 1; ++i)
     if (i < nt) issue(i);
 
+  // (rows past the last read it and store nothing)
   const int r0 = (rt * NW + wave) * 32, r = r0 + col;
-  const Row rw = row_of(a, min(r, a.R - 1), kvh);
-  typename Tl::Frag q, g;
-  Tl::load(q, row_ptr<T>(a.q, a.qs, b, rw), half);
-  Tl::load(g, row_ptr<T>(a.dout, a.gs, b, rw), half);
-  float lse2, ndelta;
-  {
-    typename Tl::Frag out;
-    Tl::load(out, row_ptr<T>(a.out, a.os, b, rw), half);
-    const float lraw = a.lse[(int64_t)bk * a.R + min(r, a.R - 1)];
-    wait_vmem_all();
-    const float d = Tl::dot(out, g);
-    ndelta = -(d + __shfl_xor(d, 32));
-    lse2 = r < a.R && lraw != -__builtin_inff() ? lraw * kLog2e : __builtin_inff();
-  }
-  if (half == 0) {
-    const int64_t at = (int64_t)bk * a.Rp + r;
-    a.stats[at] = lse2;
-    a.stats[(int64_t)a.B * a.kv * a.Rp + at] = ndelta;
-  }
+  typename Tl::Frag q;
+  Tl::load(q, row_ptr<T>(a.q, a.qs, b, row_of(a, min(r, a.R - 1), kvh)), half);
   Tl tl;
   tl.init(lane);
-  f32x16 acc[NDB];
-#pragma unroll
-  for (int db = 0; db < NDB; ++db) acc[db] = f32x16{};
+  Softmax<T, D> sm;
+  sm.init();
+  wait_vmem_all();
 
   for (int i = 0; i < nt; ++i) {
     wait_tiles_then_barrier<Copy::LPT, RING - 2>(min(RING - 2, nt - 1 - i));
     if (i + RING - 1 < nt) issue(i + RING - 1);
     const char *st = lds + (i % RING) * STAGE;
-    const int left = len - i * BN;
+    sm.tile(tl, st, st + BN * Tl::ROW, q, a.scale_log2, len - i * BN, half);
+  }
+  const float l = sm.l + __shfl_xor(sm.l, 32);
+  wait_then_barrier<0>();   // every wave is done with the ring
+  if (a.lse && half == 0 && r < a.R) a.lse[(int64_t)bk * a.R + r] = lse_of(sm.m, l);
+  // each lane's factor goes into its own row before the rows are staged
+  const float inv = inv_of(l);
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) sm.o[db] *= inv;
+  store_rows<T, D>(lds + wave * AREA, sm.o, 1.f, lane, [&](int i) {
+    return r0 + i < a.R ? row_ptr<T>(a.out, a.os, b, row_of(a, r0 + i, kvh)) : nullptr;
+  });
+}
+
+// Few rows: a workgroup takes 32 rows, and its four waves go through the keys' tiles by
+// turns, each with a ring of its own (no barrier until their sums are joined through
+// LDS); the keys may be split over workgroups as well, a.per of them each, so that the
+// splits of a long and a short batch element are of one size and those past its end do
+// nothing. Bound by the states' bytes: 128 KiB per CU are in flight.
+template <typename T, int D>
+struct FewRows {
+  using Tl = Tile<T, D>;
+  static constexpr int STAGE = 2 * BN * Tl::ROW, RING = 8 * STAGE <= 128 * 1024 ? 2 : 1;
+  static constexpr int PER = (16 * Tl::NDB + 2) * 64 * 4;   // a wave's sums, maxima and O
+  static constexpr int LDSB = 4 * RING * STAGE;
+  static_assert(3 * PER + 32 * (Tl::ROW + 16) <= LDSB, "the waves' sums and the rows' staging must fit the rings");
+  using Copy = KvCopy<T, D, 1>;
+  static_assert(Copy::LPT < 64, "vmcnt range");
+  const char *K, *V;
+  uint32_t kr, vr;
+  int k0, k1, nt;   // keys [k0, k1), this wave's tiles: wave, wave + 4, ...
+  char *ring;
+  __device__ __forceinline__ void init(const CrossArgs &a, char *lds, int sp, int b, int kvh, int wave) {
+    const int len = keys_of(a, b);
+    k0 = sp * a.per;
+    k1 = min(k0 + a.per, len);
+    const int tiles = k1 > k0 ? (k1 - k0 + BN - 1) / BN : 0;
+    nt = (tiles - wave + 3) / 4;
+    K = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head);
+    V = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + b * a.vs.batch + kvh * a.vs.head);
+    kr = (uint32_t)a.ks.row * sizeof(T);
+    vr = (uint32_t)a.vs.row * sizeof(T);
+    ring = lds + wave * RING * STAGE;
+  }
+  __device__ __forceinline__ int first(int i, int wave) const { return k0 + (4 * i + wave) * BN; }
+  __device__ __forceinline__ void issue(int i, int wave, int lane) const {
+    const int at = first(i, wave);
+    Copy::issue(K + (int64_t)at * kr, V + (int64_t)at * vr, kr, vr, k1 - 1 - at, ring + (i % RING) * STAGE, 0, lane);
+  }
+  // f(stage, keys from its first on) for each of the wave's tiles
+  template <class F>
+  __device__ __forceinline__ void walk(int wave, int lane, F f) const {
+    for (int i = 0; i < nt; ++i) {
+      // (no barrier: the wave reads only what it copied itself)
+      if (RING == 2 && i + 1 < nt) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Copy::LPT) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      f(ring + (i % RING) * STAGE, k1 - first(i, wave));
+      if (i + RING < nt) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // its reads of the stage are done
+        issue(i + RING, wave, lane);
+      }
+    }
+  }
+  __device__ __forceinline__ void start(int wave, int lane) const {
+#pragma unroll
+    for (int i = 0; i < RING; ++i)
+      if (i < nt) issue(i, wave, lane);
+  }
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 1) cross_fwd_few(CrossArgs a) {
+  using Tl = Tile<T, D>;
+  using Few = FewRows<T, D>;
+  constexpr int NDB = Tl::NDB;
+  __shared__ __attribute__((aligned(16))) char lds[Few::LDSB];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int logical = deal(blockIdx.x, a.unit);
+  if (logical >= a.total) return;
+  const int rt = logical % a.n_rtiles, t = logical / a.n_rtiles;
+  const int sp = t % a.splits, bk = t / a.splits, b = bk / a.kv, kvh = bk - b * a.kv;
+  Few few;
+  few.init(a, lds, sp, b, kvh, wave);
+  if (few.k0 >= few.k1 && a.splits > 1) return;
+  few.start(wave, lane);
+  const int r0 = rt * 32, r = r0 + col;
+  typename Tl::Frag q;
+  Tl::load(q, row_ptr<T>(a.q, a.qs, b, row_of(a, min(r, a.R - 1), kvh)), half);
+  Tl tl;
+  tl.init(lane);
+  Softmax<T, D> sm;
+  sm.init();
+  few.walk(wave, lane, [&](const char *st, int left) {
+    sm.tile(tl, st, st + BN * Tl::ROW, q, a.scale_log2, left, half);
+  });
+  const float m = sm.m;   // (no tile: -inf, and zeros)
+  float l = sm.l + __shfl_xor(sm.l, 32);
+
+  // Waves 1 to 3 hand over O, m and l.
+  wait_then_barrier<0>();
+  float *ex = reinterpret_cast<float *>(lds) + lane;
+  auto at = [&](int w, int i) { return (w - 1) * (Few::PER / 4) + i * 64; };
+  if (wave) {
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) ex[at(wave, 16 * db + v)] = sm.o[db][v];
+    ex[at(wave, 16 * NDB)] = m;
+    ex[at(wave, 16 * NDB + 1)] = l;
+  }
+  wait_then_barrier<0>();
+  if (wave) return;
+  float top = m;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) top = fmaxf(top, ex[at(w, 16 * NDB)]);
+  const float ref = top == -__builtin_inff() ? 0.f : top;
+  {
+    const float f = __builtin_amdgcn_exp2f(m - ref);
+    l *= f;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) sm.o[db] *= f;
+  }
+#pragma unroll
+  for (int w = 1; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(ex[at(w, 16 * NDB)] - ref);
+    l += f * ex[at(w, 16 * NDB + 1)];
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sm.o[db][v] = __builtin_fmaf(f, ex[at(w, 16 * db + v)], sm.o[db][v]);
+  }
+  if (a.splits > 1) {
+    const int64_t to = ((int64_t)bk * a.splits + sp) * a.R + r;
+    if (r < a.R) {
+      float *p = a.part + to * D;
+      Tl::columns(sm.o, half, [&](int c, f32x4 v) { *reinterpret_cast<f32x4 *>(p + c) = v; });
+      if (half == 0) a.part_ml[to] = make_float2(top, l);
+    }
+    return;
+  }
+  if (a.lse && half == 0 && r < a.R) a.lse[(int64_t)bk * a.R + r] = lse_of(top, l);
+  const float inv = inv_of(l);
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) sm.o[db] *= inv;
+  store_rows<T, D>(lds + 3 * Few::PER, sm.o, 1.f, lane, [&](int i) {
+    return r0 + i < a.R ? row_ptr<T>(a.out, a.os, b, row_of(a, r0 + i, kvh)) : nullptr;
+  });
+}
+
+// Up to 128 keys (a text's tokens): keys and values stay in LDS, and a workgroup's waves,
+// each for itself, go through blocks of 32 rows with the next block's queries in flight.
+// Bound by HBM (q in, out out). (16 x 6 heads of 32, 4096 rows against 77 keys.)
+// (fp32 rows of 64: 98 KiB of LDS leave one workgroup per CU)
+constexpr int short_waves(int row_bytes) { return row_bytes > 128 ? 1 : 2; }
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256, short_waves(sizeof(T) * D)) cross_fwd_short(CrossArgs a) {
+  using Tl = Tile<T, D>;
+  constexpr int NDB = Tl::NDB, STAGE = 2 * BN * Tl::ROW, AREA = 32 * (Tl::ROW + 16);
+  __shared__ __attribute__((aligned(16))) char lds[2 * STAGE + 4 * AREA];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int logical = deal(blockIdx.x, a.unit);
+  if (logical >= a.total) return;
+  const int part = logical % a.row_parts, bk = logical / a.row_parts, b = bk / a.kv, kvh = bk - b * a.kv;
+  const int len = keys_of(a, b), nt = (len + BN - 1) / BN;
+  const char *K = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head);
+  const char *V = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + b * a.vs.batch + kvh * a.vs.head);
+  const uint32_t kr = (uint32_t)a.ks.row * sizeof(T), vr = (uint32_t)a.vs.row * sizeof(T);
+  for (int i = 0; i < nt; ++i)
+    KvCopy<T, D, 4>::issue(K + (int64_t)i * BN * kr, V + (int64_t)i * BN * vr, kr, vr, len - 1 - i * BN, lds + i * STAGE, wave, lane);
+  const int nblk = (a.R + 31) / 32, step = 4 * a.row_parts;
+  int rb = part * 4 + wave;
+  auto load = [&](typename Tl::Frag &q, int blk) {
+    Tl::load(q, row_ptr<T>(a.q, a.qs, b, row_of(a, min(blk * 32 + col, a.R - 1), kvh)), half);
+  };
+  typename Tl::Frag q;
+  if (rb < nblk) load(q, rb);
+  Tl tl;
+  tl.init(lane);
+  wait_vmem_all();
+  wait_then_barrier<0>();
+  for (; rb < nblk; rb += step) {
+    typename Tl::Frag next;
+    load(next, min(rb + step, nblk - 1));
+    Softmax<T, D> sm;
+    sm.init();
+    for (int i = 0; i < nt; ++i) {
+      const char *st = lds + i * STAGE;
+      sm.tile(tl, st, st + BN * Tl::ROW, q, a.scale_log2, len - i * BN, half);
+    }
+    const float l = sm.l + __shfl_xor(sm.l, 32), inv = inv_of(l);
+    const int r0 = rb * 32;
+    if (a.lse && half == 0 && r0 + col < a.R) a.lse[(int64_t)bk * a.R + r0 + col] = lse_of(sm.m, l);
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) sm.o[db] *= inv;
+    store_rows<T, D>(lds + 2 * STAGE + wave * AREA, sm.o, 1.f, lane, [&](int i) {
+      return r0 + i < a.R ? row_ptr<T>(a.out, a.os, b, row_of(a, r0 + i, kvh)) : nullptr;
+    });
+#pragma unroll
+    for (int c = 0; c < Tl::NCH; ++c) q[c] = next[c];
+  }
+}
+
+// Joins the partial sums of the key splits. One wave per row: D / 4 lanes take four
+// columns each, 256 / D groups of them every 256 / D-th split.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) cross_join(CrossArgs a) {
+  constexpr int TPR = D / 4, SL = 64 / TPR;
+  const int lane = threadIdx.x & 63, c = lane % TPR * 4, first = lane / TPR;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= (int64_t)a.B * a.kv * a.R) return;
+  const int bk = (int)(row / a.R), r = (int)(row - (int64_t)bk * a.R), b = bk / a.kv, kvh = bk - b * a.kv;
+  const int n = (keys_of(a, b) + a.per - 1) / a.per;   // splits with keys
+  const float2 *ml = a.part_ml + (int64_t)bk * a.splits * a.R + r;
+  const float *p = a.part + ((int64_t)bk * a.splits * a.R + r) * D + c;
+  float m = -__builtin_inff();
+#pragma unroll 4
+  for (int s = first; s < n; s += SL) m = fmaxf(m, ml[(int64_t)s * a.R].x);
+#pragma unroll
+  for (int x = TPR; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
+  const float ref = m == -__builtin_inff() ? 0.f : m;
+  float l = 0.f;
+  f32x4 o = {};
+#pragma unroll 4
+  for (int s = first; s < n; s += SL) {
+    const float2 e = ml[(int64_t)s * a.R];
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(p + (int64_t)s * a.R * D);
+    const float w = __builtin_amdgcn_exp2f(e.x - ref);
+    l += w * e.y;
+    o += w * x;
+  }
+#pragma unroll
+  for (int x = TPR; x < 64; x *= 2) {
+    l += __shfl_xor(l, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], x);
+  }
+  if (first) return;
+  if (a.lse && c == 0) a.lse[(int64_t)bk * a.R + r] = lse_of(m, l);
+  put4<T>(row_ptr<T>(a.out, a.os, b, row_of(a, r, kvh)) + c, o * inv_of(l));
+}
+
+// A wave's 32 rows of the backward: q, dout and the statistics.
+template <typename T, int D>
+struct BwdRows {
+  using Tl = Tile<T, D>;
+  typename Tl::Frag q, g, out;
+  float lraw, lse2, ndelta;
+  __device__ __forceinline__ void load(const CrossArgs &a, int bk, int b, int kvh, int r, int half) {
+    const int rc = min(r, a.R - 1);   // (rows past the last read it and store nothing)
+    const Row rw = row_of(a, rc, kvh);
+    Tl::load(q, row_ptr<T>(a.q, a.qs, b, rw), half);
+    Tl::load(g, row_ptr<T>(a.dout, a.gs, b, rw), half);
+    Tl::load(out, row_ptr<T>(a.out, a.os, b, rw), half);
+    lraw = a.lse[(int64_t)bk * a.R + rc];
+  }
+  // The statistics, kept and stored for the dk / dv kernel: lse log2 e (+inf for a row
+  // without a key and for the padding of the last tile, which makes every weight
+  // exp2(s - inf) = 0) and -delta.
+  __device__ __forceinline__ void finish(const CrossArgs &a, int bk, int r, int half, bool keep = true) {
+    const float d = Tl::dot(out, g);
+    ndelta = -(d + __shfl_xor(d, 32));
+    lse2 = r < a.R && lraw != -__builtin_inff() ? lraw * kLog2e : __builtin_inff();
+    if (half == 0 && keep) {
+      const int64_t at = (int64_t)bk * a.Rp + r;
+      a.stats[at] = lse2;
+      a.stats[(int64_t)a.B * a.kv * a.Rp + at] = ndelta;
+    }
+  }
+  // acc += dS K over the `left` keys of a tile (K tile, then V tile, at st)
+  __device__ __forceinline__ void tile(const Tl &tl, const char *st, float scale, int left, int half,
+                                       f32x16 (&acc)[Tl::NDB]) const {
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       if (32 * kb >= left) break;
@@ -302,9 +534,52 @@ __global__ void __launch_bounds__(64 * NW, 2) cross_dq(CrossArgs a) {
       if (left < 32 * kb + 32) mask_tail(s, left - 32 * kb, half);
 #pragma unroll
       for (int v = 0; v < 16; ++v)
-        s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], a.scale_log2, -lse2)) * (dp[v] + ndelta);
+        s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], scale, -lse2)) * (dp[v] + ndelta);
       tl.cols_times(blk, s, acc);
     }
+  }
+};
+
+// dq, and the rows' statistics for the next kernel. Many rows: as cross_fwd.
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 2) cross_dq(CrossArgs a) {
+  using Tl = Tile<T, D>;
+  constexpr int NDB = Tl::NDB, RING = fwd_ring<T, D>(), NW = 4;
+  constexpr int STAGE = 2 * BN * Tl::ROW;
+  constexpr int AREA = 32 * (Tl::ROW + 16);
+  using Copy = KvCopy<T, D, NW>;
+  __shared__ __attribute__((aligned(16))) char lds[RING * STAGE];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int logical = deal(blockIdx.x, a.unit);
+  if (logical >= a.total) return;
+  const int rt = logical % a.n_rtiles, bk = logical / a.n_rtiles, b = bk / a.kv, kvh = bk - b * a.kv;
+  const int len = keys_of(a, b), nt = (len + BN - 1) / BN;
+  const char *K = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head);
+  const char *V = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + b * a.vs.batch + kvh * a.vs.head);
+  const uint32_t kr = (uint32_t)a.ks.row * sizeof(T), vr = (uint32_t)a.vs.row * sizeof(T);
+  auto issue = [&](int i) {
+    const int at = i * BN;
+    Copy::issue(K + (int64_t)at * kr, V + (int64_t)at * vr, kr, vr, len - 1 - at, lds + (i % RING) * STAGE, wave, lane);
+  };
+#pragma unroll
+  for (int i = 0; i < RING - 1; ++i)
+    if (i < nt) issue(i);
+  const int r0 = (rt * NW + wave) * 32;
+  BwdRows<T, D> rows;
+  rows.load(a, bk, b, kvh, r0 + col, half);
+  wait_vmem_all();
+  rows.finish(a, bk, r0 + col, half);
+  Tl tl;
+  tl.init(lane);
+  f32x16 acc[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) acc[db] = f32x16{};
+  for (int i = 0; i < nt; ++i) {
+    wait_tiles_then_barrier<Copy::LPT, RING - 2>(min(RING - 2, nt - 1 - i));
+    if (i + RING - 1 < nt) issue(i + RING - 1);
+    rows.tile(tl, lds + (i % RING) * STAGE, a.scale_log2, len - i * BN, half, acc);
   }
   wait_then_barrier<0>();
   store_rows<T, D>(lds + wave * AREA, acc, a.scale, lane, [&](int i) {
@@ -312,53 +587,150 @@ __global__ void __launch_bounds__(64 * NW, 2) cross_dq(CrossArgs a) {
   });
 }
 
-// dk and dv of 64 keys. Wave w takes the 32 keys of block w % 2 against half w / 2 of
-// the rows of every step (RB blocks of 32); the halves are added through LDS.
-template <typename T, int D, int RB>
-__global__ void __launch_bounds__(256, 2) cross_dkdv(CrossArgs a) {
+// Few rows: as cross_fwd_few.
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 1) cross_dq_few(CrossArgs a) {
   using Tl = Tile<T, D>;
-  constexpr int NDB = Tl::NDB, BR = 64 * RB;   // rows per step
+  using Few = FewRows<T, D>;
+  constexpr int NDB = Tl::NDB;
+  __shared__ __attribute__((aligned(16))) char lds[Few::LDSB];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int logical = deal(blockIdx.x, a.unit);
+  if (logical >= a.total) return;
+  const int rt = logical % a.n_rtiles, bk = logical / a.n_rtiles, b = bk / a.kv, kvh = bk - b * a.kv;
+  Few few;
+  few.init(a, lds, 0, b, kvh, wave);
+  few.start(wave, lane);
+  const int r0 = rt * 32;
+  BwdRows<T, D> rows;
+  rows.load(a, bk, b, kvh, r0 + col, half);
+  rows.finish(a, bk, r0 + col, half, wave == 0);
+  Tl tl;
+  tl.init(lane);
+  f32x16 acc[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) acc[db] = f32x16{};
+  few.walk(wave, lane, [&](const char *st, int left) { rows.tile(tl, st, a.scale_log2, left, half, acc); });
+  wait_then_barrier<0>();
+  float *ex = reinterpret_cast<float *>(lds) + lane;
+  auto at = [&](int w, int i) { return (w - 1) * (Few::PER / 4) + i * 64; };
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+      if (wave) ex[at(wave, 16 * db + v)] = acc[db][v];
+  wait_then_barrier<0>();
+  if (wave) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w)
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[db][v] += ex[at(w, 16 * db + v)];
+  store_rows<T, D>(lds + 3 * Few::PER, acc, a.scale, lane, [&](int i) {
+    return r0 + i < a.R ? row_ptr<T>(a.dq, a.dqs, b, row_of(a, r0 + i, kvh)) : nullptr;
+  });
+}
+
+// The same for up to 128 keys, which stay in LDS: as cross_fwd_short, with the next
+// block's q, dout, out and lse in flight.
+template <typename T, int D>
+__global__ void __launch_bounds__(256, short_waves(sizeof(T) * D)) cross_dq_short(CrossArgs a) {
+  using Tl = Tile<T, D>;
+  constexpr int NDB = Tl::NDB, STAGE = 2 * BN * Tl::ROW, AREA = 32 * (Tl::ROW + 16);
+  __shared__ __attribute__((aligned(16))) char lds[2 * STAGE + 4 * AREA];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int logical = deal(blockIdx.x, a.unit);
+  if (logical >= a.total) return;
+  const int part = logical % a.row_parts, bk = logical / a.row_parts, b = bk / a.kv, kvh = bk - b * a.kv;
+  const int len = keys_of(a, b), nt = (len + BN - 1) / BN;
+  const char *K = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head);
+  const char *V = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + b * a.vs.batch + kvh * a.vs.head);
+  const uint32_t kr = (uint32_t)a.ks.row * sizeof(T), vr = (uint32_t)a.vs.row * sizeof(T);
+  for (int i = 0; i < nt; ++i)
+    KvCopy<T, D, 4>::issue(K + (int64_t)i * BN * kr, V + (int64_t)i * BN * vr, kr, vr, len - 1 - i * BN, lds + i * STAGE, wave, lane);
+  // (blocks up to the padded end of the list: their statistics are read by the next kernel)
+  const int nblk = a.Rp / 32, step = 4 * a.row_parts;
+  int rb = part * 4 + wave;
+  BwdRows<T, D> rows;
+  rows.load(a, bk, b, kvh, min(rb, nblk - 1) * 32 + col, half);
+  Tl tl;
+  tl.init(lane);
+  wait_vmem_all();
+  wait_then_barrier<0>();
+  for (; rb < nblk; rb += step) {
+    const int r0 = rb * 32;
+    rows.finish(a, bk, r0 + col, half);
+    BwdRows<T, D> next;
+    next.load(a, bk, b, kvh, min(rb + step, nblk - 1) * 32 + col, half);
+    f32x16 acc[NDB];
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) acc[db] = f32x16{};
+    for (int i = 0; i < nt; ++i) rows.tile(tl, lds + i * STAGE, a.scale_log2, len - i * BN, half, acc);
+    store_rows<T, D>(lds + 2 * STAGE + wave * AREA, acc, a.scale, lane, [&](int i) {
+      return r0 + i < a.R ? row_ptr<T>(a.dq, a.dqs, b, row_of(a, r0 + i, kvh)) : nullptr;
+    });
+    rows = next;
+  }
+}
+
+// dk and dv of KB blocks of 32 keys: wave w takes the keys of block w % KB against part
+// w / KB of the rows of every step (RB blocks of 32; RH parts). Rows come into an LDS
+// ring by the 16-byte DMA; with RH = 2 the parts are added through LDS at the end.
+template <typename T, int D, int KB, int RH, int RB>
+__global__ void __launch_bounds__(64 * KB * RH, 2) cross_dkdv(CrossArgs a) {
+  using Tl = Tile<T, D>;
+  constexpr int NDB = Tl::NDB, NW = KB * RH, BR = 32 * RB * RH;   // waves, rows per step
   constexpr int TILE = BR * Tl::ROW;
   constexpr int STAT = 2 * TILE, STAGE = STAT + BR * 8;
-  constexpr int CPW = BR * Tl::CPR / 256;
+  constexpr int CPW = BR * Tl::CPR / (64 * NW);
+  constexpr int RING = NW == 8 && 3 * STAGE <= 160 * 1024 ? 3 : 2;
+  constexpr int SW = BR * 2 / 64;                  // waves that copy statistics
+  constexpr int LPT = 2 * CPW + 1;
   constexpr int AREA = 32 * (Tl::ROW + 16);
-  constexpr int XCH = 2 * 2 * NDB * 16 * 64 * 4;
-  constexpr int LDSB = 2 * STAGE > XCH ? 2 * STAGE : XCH;
-  static_assert(4 * AREA <= LDSB, "the rows' staging must fit the ring");
+  constexpr int XCH = KB * 2 * NDB * 16 * 64 * 4;
+  constexpr int LDSB = RH == 2 && RING * STAGE < XCH ? XCH : RING * STAGE;
+  static_assert(NW * AREA <= LDSB && SW <= NW, "staging, statistics");
+  static_assert(BR * Tl::CPR % (64 * NW) == 0, "copies must split evenly");
   __shared__ __attribute__((aligned(16))) char lds[LDSB];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 31, half = lane >> 5, kb = wave & 1, rh = wave >> 1;
-  const int logical = xcd_remap(blockIdx.x, gridDim.x);
+  const int col = lane & 31, half = lane >> 5, kb = wave % KB, rh = wave / KB;
+  const int logical = deal(blockIdx.x, a.unit);
+  if (logical >= a.total) return;
   const int kt = logical % a.n_ktiles, t = logical / a.n_ktiles;
   const int sp = t % a.splits, bk = t / a.splits, b = bk / a.kv, kvh = bk - b * a.kv;
   const int len = keys_of(a, b);
-  const int kpos = kt * BN + 32 * kb + col;
+  const int j0 = (kt * KB + kb) * 32, kpos = j0 + col;   // this wave's first key, this lane's
   // (no key of the tile is seen: zeros, which the joining launch knows by itself)
-  if (kt * BN >= len && a.splits > 1) return;
+  if (kt * KB * 32 >= len && a.splits > 1) return;
 
-  // This split's rows [r0, r1): whole steps but for the last.
+  // This split's rows: whole steps.
   const int steps = (a.R + BR - 1) / BR, per = (steps + a.splits - 1) / a.splits;
-  const int i0 = min(sp * per, steps), i1 = kt * BN < len ? min(i0 + per, steps) : i0;
+  const int i0 = min(sp * per, steps), i1 = kt * KB * 32 < len ? min(i0 + per, steps) : i0;
   const float *S = a.stats + (int64_t)bk * a.Rp;
   const int64_t dofs = (int64_t)a.B * a.kv * a.Rp;   // from lse to -delta
   auto issue = [&](int i) {
-    char *stage = lds + (i & 1) * STAGE;
+    char *stage = lds + (i - i0) % RING * STAGE;
 #pragma unroll
     for (int j = 0; j < CPW; ++j) {
-      const int p = (j * 4 + wave) * 64 + lane, rr = p / Tl::CPR, c = (p % Tl::CPR) ^ Tl::swz(rr);
+      const int p = (j * NW + wave) * 64 + lane, rr = p / Tl::CPR, c = (p % Tl::CPR) ^ Tl::swz(rr);
       // (rows past the last read it; their statistics make their weights 0)
       const Row rw = row_of(a, min(i * BR + rr, a.R - 1), kvh);
-      lds_dma16(reinterpret_cast<const char *>(row_ptr<T>(a.q, a.qs, b, rw)) + c * 16, lds_addr(stage + (j * 4 + wave) * 1024));
+      lds_dma16(reinterpret_cast<const char *>(row_ptr<T>(a.q, a.qs, b, rw)) + c * 16, lds_addr(stage + (j * NW + wave) * 1024));
       lds_dma16(reinterpret_cast<const char *>(row_ptr<T>(a.dout, a.gs, b, rw)) + c * 16,
-                lds_addr(stage + TILE + (j * 4 + wave) * 1024));
+                lds_addr(stage + TILE + (j * NW + wave) * 1024));
     }
-    if (wave < 2 * RB) {   // 64 rows' lse, or -delta, per wave
-      const int which = wave / RB, part = wave % RB;
-      lds_dma4(S + which * dofs + i * BR + part * 64 + lane, lds_addr(stage + STAT + which * BR * 4 + part * 256));
-    }
+    // 64 rows' lse, or -delta, per wave (the waves past them copy the last again, so that
+    // all have the same number in flight)
+    const int w = min(wave, SW - 1), which = w / (SW / 2), part = w % (SW / 2);
+    lds_dma4(S + which * dofs + i * BR + part * 64 + lane, lds_addr(stage + STAT + which * BR * 4 + part * 256));
   };
-  if (i0 < i1) issue(i0);
+#pragma unroll
+  for (int i = 0; i < RING - 1; ++i)
+    if (i0 + i < i1) issue(i0 + i);
 
   const int64_t krow = min(kpos, max(len - 1, 0));   // (unseen keys: not stored)
   typename Tl::Frag k, v;
@@ -372,9 +744,10 @@ __global__ void __launch_bounds__(256, 2) cross_dkdv(CrossArgs a) {
   wait_vmem_all();
 
   for (int i = i0; i < i1; ++i) {
-    wait_then_barrier<0>();
-    if (i + 1 < i1) issue(i + 1);
-    const char *st = lds + (i & 1) * STAGE;
+    wait_tiles_then_barrier<LPT, RING - 2>(min(RING - 2, i1 - 1 - i));
+    if (i + RING - 1 < i1) issue(i + RING - 1);
+    if (j0 >= len) continue;   // (none of the wave's keys is seen)
+    const char *st = lds + (i - i0) % RING * STAGE;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const int first = (rh * RB + rb) * 32;
@@ -399,37 +772,42 @@ __global__ void __launch_bounds__(256, 2) cross_dkdv(CrossArgs a) {
     }
   }
 
-  // Half 1 hands its dk to half 0, half 0 its dv to half 1; then half 0 has dk, half 1 dv.
-  wait_then_barrier<0>();
-  float *xch = reinterpret_cast<float *>(lds);
-  auto at = [&](int which, int db, int e) { return (((kb * 2 + which) * NDB + db) * 16 + e) * 64 + lane; };
+  // RH = 2: part 1 hands its dk to part 0 and part 0 its dv to part 1; then each holds
+  // one sum. RH = 1: both are here.
+  wait_then_barrier<0>();   // every wave is done with the ring
+  if constexpr (RH == 2) {
+    float *xch = reinterpret_cast<float *>(lds);
+    auto at = [&](int which, int db, int e) { return (((kb * 2 + which) * NDB + db) * 16 + e) * 64 + lane; };
 #pragma unroll
-  for (int db = 0; db < NDB; ++db)
+    for (int db = 0; db < NDB; ++db)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) xch[at(rh, db, e)] = rh ? dk[db][e] : dv[db][e];
-  wait_then_barrier<0>();
-  f32x16 sum[NDB];
+      for (int e = 0; e < 16; ++e) xch[at(rh, db, e)] = rh ? dk[db][e] : dv[db][e];
+    wait_then_barrier<0>();
 #pragma unroll
-  for (int db = 0; db < NDB; ++db)
+    for (int db = 0; db < NDB; ++db)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sum[db][e] = (rh ? dv[db][e] : dk[db][e]) + xch[at(1 - rh, db, e)];
-  wait_then_barrier<0>();
-  if (a.splits > 1) {
-    if (kpos < len) {
-      float *p = a.part + ((((int64_t)sp * a.B * a.kv + bk) * a.M + kpos) * 2 + rh) * D;
-      Tl::columns(sum, half, [&](int c, f32x4 x) { *reinterpret_cast<f32x4 *>(p + c) = x; });
+      for (int e = 0; e < 16; ++e) dk[db][e] = (rh ? dv[db][e] : dk[db][e]) + xch[at(1 - rh, db, e)];
+    wait_then_barrier<0>();
+  }
+  auto put = [&](f32x16 (&sum)[NDB], int which) {
+    if (a.splits > 1) {
+      if (kpos < len) {
+        float *p = a.part + ((((int64_t)sp * a.B * a.kv + bk) * a.M + kpos) * 2 + which) * D;
+        Tl::columns(sum, half, [&](int c, f32x4 x) { *reinterpret_cast<f32x4 *>(p + c) = x; });
+      }
+      return;
     }
-    return;
-  }
-  if (kpos >= len) {
+    if (kpos >= len) {
 #pragma unroll
-    for (int db = 0; db < NDB; ++db) sum[db] = f32x16{};
-  }
-  const CrossStride &os = rh ? a.dvs : a.dks;
-  T *dst = static_cast<T *>(rh ? a.dv : a.dk) + b * os.batch + kvh * os.head;
-  const int j0 = kt * BN + 32 * kb;
-  store_rows<T, D>(lds + wave * AREA, sum, rh ? 1.f : a.scale, lane,
-                   [&](int i) { return j0 + i < a.M ? dst + (j0 + i) * os.row : nullptr; });
+      for (int db = 0; db < NDB; ++db) sum[db] = f32x16{};
+    }
+    const CrossStride &os = which ? a.dvs : a.dks;
+    T *dst = static_cast<T *>(which ? a.dv : a.dk) + b * os.batch + kvh * os.head;
+    store_rows<T, D>(lds + wave * AREA, sum, which ? 1.f : a.scale, lane,
+                     [&](int i) { return j0 + i < a.M ? dst + (j0 + i) * os.row : nullptr; });
+  };
+  put(dk, RH == 2 ? rh : 0);
+  if constexpr (RH == 1) put(dv, 1);
 }
 
 // Adds the partial sums of the row splits: one thread per key, gradient and four columns.
@@ -451,35 +829,75 @@ __global__ void __launch_bounds__(256) cross_sum(CrossArgs a) {
   put4<T>(dst + c, sum * (which ? 1.f : a.scale));
 }
 
-// Row tiles of one wave where a list's rows fit one: its workgroups are then single
-// waves, each with a ring of its own.
-int fwd_waves(const CrossArgs &a) { return a.R <= 32 ? 1 : 4; }
+// Tiles of 32 rows, the keys shared by the waves, where tiles of 128 would leave CUs
+// without work.
+bool few_rows(const CrossArgs &a) { return (int64_t)a.B * a.kv * ((a.R + 127) / 128) < device_cu_count(); }
+
+// Keys that stay in LDS, against rows enough that they are met more than once.
+bool keys_stay(const CrossArgs &a) { return a.M <= 128 && a.R > 32; }
+
+// Blocks of 32 keys of a dk / dv workgroup: four (eight waves, one workgroup per CU)
+// where those fill the CUs, runs of 128 rows included.
+int kv_blocks(const CrossArgs &a) {
+  const int64_t most = (int64_t)a.B * a.kv * ((a.M + 127) / 128) * ((a.R + 127) / 128);
+  return a.M > 64 && most >= device_cu_count() ? 4 : 2;
+}
+
+// Grid of `total` pieces of work, dealt to the XCDs in runs.
+dim3 deal_grid(CrossArgs &a, int64_t total) {
+  a.total = (int32_t)total;
+  a.unit = (int32_t)std::max<int64_t>(1, std::min<int64_t>(32, total / 32));
+  const int64_t round = 8 * a.unit;
+  return dim3((uint32_t)((total + round - 1) / round * round));
+}
 
 template <typename T, int D>
 hipError_t fwd(CrossArgs &a, hipStream_t s) {
-  const int nw = fwd_waves(a);
-  a.n_rtiles = (a.R + 32 * nw - 1) / (32 * nw);
-  const dim3 grid((uint32_t)((int64_t)a.B * a.kv * a.n_rtiles * a.splits));
-  if (nw == 1) hipLaunchKernelGGL((cross_fwd<T, D, 1>), grid, dim3(64), 0, s, a);
-  else hipLaunchKernelGGL((cross_fwd<T, D, 4>), grid, dim3(256), 0, s, a);
+  const int64_t bk = (int64_t)a.B * a.kv;
+  if (keys_stay(a)) {
+    const dim3 grid = deal_grid(a, bk * a.row_parts);
+    hipLaunchKernelGGL((cross_fwd_short<T, D>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  if (!few_rows(a)) {
+    a.n_rtiles = (a.R + 127) / 128;
+    const dim3 grid = deal_grid(a, bk * a.n_rtiles);
+    hipLaunchKernelGGL((cross_fwd<T, D>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  a.n_rtiles = (a.R + 31) / 32;
+  const dim3 grid = deal_grid(a, bk * a.n_rtiles * a.splits);
+  hipLaunchKernelGGL((cross_fwd_few<T, D>), grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t n = (int64_t)a.B * a.kv * a.R * (D / 4);
-  hipLaunchKernelGGL((cross_join<T, D>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((cross_join<T, D>), dim3((uint32_t)((bk * a.R + 3) / 4)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t bwd(CrossArgs &a, hipStream_t s) {
   constexpr int RB = sizeof(T) == 4 ? 1 : 2;
-  a.n_rtiles = (a.R + 127) / 128;
-  hipLaunchKernelGGL((cross_dq<T, D, 4>), dim3((uint32_t)((int64_t)a.B * a.kv * a.n_rtiles)), dim3(256), 0, s, a);
+  const int64_t bk = (int64_t)a.B * a.kv;
+  if (keys_stay(a)) {
+    const dim3 grid = deal_grid(a, bk * a.row_parts);
+    hipLaunchKernelGGL((cross_dq_short<T, D>), grid, dim3(256), 0, s, a);
+  } else if (few_rows(a)) {
+    a.n_rtiles = a.Rp / 32;   // (the padded rows' statistics as well)
+    const dim3 grid = deal_grid(a, bk * a.n_rtiles);
+    hipLaunchKernelGGL((cross_dq_few<T, D>), grid, dim3(256), 0, s, a);
+  } else {
+    a.n_rtiles = a.Rp / 128;
+    const dim3 grid = deal_grid(a, bk * a.n_rtiles);
+    hipLaunchKernelGGL((cross_dq<T, D>), grid, dim3(256), 0, s, a);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((cross_dkdv<T, D, RB>), dim3((uint32_t)((int64_t)a.B * a.kv * a.n_ktiles * a.splits)), dim3(256), 0, s, a);
+  const dim3 grid = deal_grid(a, bk * a.n_ktiles * a.splits);
+  if (kv_blocks(a) == 2) hipLaunchKernelGGL((cross_dkdv<T, D, 2, 2, RB>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((cross_dkdv<T, D, 4, 2, RB>), grid, dim3(512), 0, s, a);
   e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t n = (int64_t)a.B * a.kv * a.M * 2 * (D / 4);
+  const int64_t n = bk * a.M * 2 * (D / 4);
   hipLaunchKernelGGL((cross_sum<T, D>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
@@ -488,18 +906,35 @@ int up_to(int64_t want, int64_t most) { return (int)std::max<int64_t>(1, std::mi
 
 }  // namespace
 
-// Key splits of the forward: enough workgroups to fill the chip with 8 waves per CU,
-// but at least two tiles of keys each.
-int cross_fwd_splits(const CrossArgs &a) {
-  const int nw = fwd_waves(a);
-  const int64_t wgs = (int64_t)a.B * a.kv * ((a.R + 32 * nw - 1) / (32 * nw));
-  return up_to((int64_t)device_cu_count() * 8 / nw / wgs, (a.M + 2 * BN - 1) / (2 * BN));
+// How the rows are shared out where the keys stay in LDS: four workgroups per CU, a block
+// of rows or more for each wave.
+static void share_rows(CrossArgs &a) {
+  a.row_parts = up_to(4 * (int64_t)device_cu_count() / ((int64_t)a.B * a.kv), (a.R + 127) / 128);
 }
 
-// Row splits of dk and dv: two workgroups per CU, at least four steps of 64 rows each.
-int cross_bwd_splits(const CrossArgs &a) {
-  const int64_t wgs = (int64_t)a.B * a.kv * ((a.M + BN - 1) / BN);
-  return up_to((int64_t)device_cu_count() * 2 / wgs, (a.R + 255) / 256);
+// Key splits of the forward: one workgroup per CU (its LDS is full), of at least eight
+// tiles each.
+bool cross_fwd_plan(CrossArgs &a) {
+  a.splits = 1;
+  a.per = (a.M + BN - 1) / BN * BN;
+  share_rows(a);
+  if (keys_stay(a) || !few_rows(a)) return false;
+  const int64_t wgs = (int64_t)a.B * a.kv * ((a.R + 31) / 32), tiles = (a.M + BN - 1) / BN;
+  const int splits = up_to(device_cu_count() / wgs, (tiles + 7) / 8);
+  a.per = (int)((tiles + splits - 1) / splits) * BN;
+  a.splits = (a.M + a.per - 1) / a.per;
+  return a.splits > 1;
+}
+
+// Row splits of dk and dv: eight waves per CU, at least 128 rows each.
+bool cross_bwd_plan(CrossArgs &a) {
+  a.splits = 1;
+  a.per = (a.M + BN - 1) / BN * BN;
+  share_rows(a);
+  const int kb = kv_blocks(a);
+  a.n_ktiles = (a.M + 32 * kb - 1) / (32 * kb);
+  a.splits = up_to((int64_t)device_cu_count() * (kb == 2 ? 2 : 1) / ((int64_t)a.B * a.kv * a.n_ktiles), (a.R + 127) / 128);
+  return a.splits > 1;
 }
 
 hipError_t launch_cross_fwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s) {

@@ -205,13 +205,17 @@ struct CrossArgs {
   float *stats;                // backward: lse log2 e of B * kv lists of Rp rows, then -delta of them
   float *part;                 // partial sums of the splits
   float2 *part_ml;             // forward: their maxima and sums
-  int32_t B, heads, kv, G, N, M, R, Rp, n_ktiles, splits;
-  int32_t n_rtiles;            // set by the launchers
+  int32_t B, heads, kv, G, N, M, R, Rp;
+  // set by the plans: splits of the keys (forward; keys of each) or of the rows (backward),
+  // workgroups that share a list's rows where the keys stay in LDS, dk / dv key tiles
+  int32_t splits, per, row_parts, n_ktiles;
+  int32_t n_rtiles, total, unit;   // set by the launchers: row tiles, pieces of work, run dealt to an XCD
   FastDiv ndiv;                // division by N
   float scale, scale_log2;
 };
-int cross_fwd_splits(const CrossArgs &a);   // from B, kv, R, M
-int cross_bwd_splits(const CrossArgs &a);
+// Share out the work, from B, kv, R and M; true: partial sums go to a workspace.
+bool cross_fwd_plan(CrossArgs &a);
+bool cross_bwd_plan(CrossArgs &a);
 hipError_t launch_cross_fwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s);
 hipError_t launch_cross_bwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s);
 
