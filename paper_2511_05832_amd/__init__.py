@@ -33,7 +33,6 @@ import ctypes
 import math
 import os
 import threading
-from contextlib import nullcontext
 from typing import Optional, Tuple
 
 import torch
@@ -666,18 +665,36 @@ def out_proj(o: torch.Tensor, w_proj: torch.Tensor, out: Optional[torch.Tensor] 
 # Operators around the attention. Tensors of one call are on one GPU; the call runs
 # there, on that GPU's current stream, whatever the current device is.
 
-def _call(t: torch.Tensor, fn, *args):
-    """fn(*args, stream) on t's device and its current stream."""
-    if t.get_device() == torch.cuda.current_device():
-        _check(fn(*args, _stream(t)))
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _on_device_of(t: torch.Tensor, fn, *args):
+    """fn(*args) with t's device current."""
+    if t.get_device() == _current_device():
+        _check(fn(*args))
     else:
         with torch.cuda.device(t.device):
-            _check(fn(*args, _stream(t)))
+            _check(fn(*args))
+
+
+def _call(t: torch.Tensor, fn, *args):
+    """fn(*args, stream) on t's device and its current stream."""
+    _on_device_of(t, fn, *args, _stream(t))
+
+
+def _new_rows(t: torch.Tensor) -> View:
+    """The view of a [B, heads, N, d] tensor that this module has made."""
+    b, h, n, _ = t.stride()
+    return View(t.data_ptr(), b, h, n)
 
 
 def _rows(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> View:
     """The view of a [B, heads, N, d] tensor whose rows are contiguous; ``like``: a
     tensor that it shares device and dtype with."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 4:   # (the usual case in one test)
+        b, h, n, e = t.stride()
+        if e == 1 and (like is None or (t.dtype == like.dtype and t.get_device() == like.get_device())):
+            return View(t.data_ptr(), b, h, n)
     if not isinstance(t, torch.Tensor):
         raise HLAError(HLA_ERR_INVALID_ARG, f"{name} must be a tensor")
     if not t.is_cuda:
@@ -687,10 +704,19 @@ def _rows(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> Vi
     if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device()):
         raise HLAError(HLA_ERR_INVALID_ARG, f"{name} is {t.dtype} on {t.device}, expected {like.dtype} "
                                             f"on {like.device}")
-    b, h, n, e = t.stride()
-    if e != 1 and t.shape[3] != 1:
-        raise HLAError(HLA_ERR_INVALID_ARG, f"{name}: the last dimension must be contiguous")
-    return View(t.data_ptr(), b, h, n)
+    raise HLAError(HLA_ERR_INVALID_ARG, f"{name}: the last dimension must be contiguous")
+
+
+def _rows_like(t: Optional[torch.Tensor], name: str, like: torch.Tensor):
+    """An output of the shape of ``like`` (default: a new tensor, laid out like it) and its
+    view."""
+    if t is None:
+        t = torch.empty_like(like)
+        return t, _new_rows(t)
+    view = _rows(t, name, like)
+    if t.shape != like.shape:
+        raise HLAError(HLA_ERR_INVALID_ARG, f"{name} must be {tuple(like.shape)}, got {tuple(t.shape)}")
+    return t, view
 
 
 def _require_on(t: torch.Tensor, name: str, like: torch.Tensor, dtype: torch.dtype):
@@ -754,31 +780,23 @@ def rope(q: torch.Tensor, freqs: torch.Tensor, k: Optional[torch.Tensor] = None,
     B, heads, N, d = q.shape
     _require_on(freqs, "freqs", q, torch.float64)
     kv_heads = 0
-    if q_out is None:
-        q_out = q.new_empty(q.shape)
-    elif q_out.shape != q.shape:
-        raise HLAError(HLA_ERR_INVALID_ARG, "q_out must have q's shape")
+    q_out, qov = _rows_like(q_out, "q_out", q)
     kv = kov = None
     if k is not None:
         kv = _rows(k, "k", q)
         kv_heads = k.shape[1]
         if k.shape[0] != B or k.shape[2] != N or k.shape[3] != d:
             raise HLAError(HLA_ERR_INVALID_ARG, f"k must be [{B}, kv_heads, {N}, {d}], got {tuple(k.shape)}")
-        if k_out is None:
-            k_out = k.new_empty(k.shape)
-        elif k_out.shape != k.shape:
-            raise HLAError(HLA_ERR_INVALID_ARG, "k_out must have k's shape")
-        kov = _rows(k_out, "k_out", q)
+        k_out, kov = _rows_like(k_out, "k_out", k)
     stride = 0
     if pos is not None:
         _require_on(pos, "pos", q, torch.int32)
-        if tuple(pos.shape) == (B, N):
+        if pos.shape == (B, N):
             stride = N
-        elif tuple(pos.shape) != (N,):
+        elif pos.shape != (N,):
             raise HLAError(HLA_ERR_INVALID_ARG, f"pos must be [{N}] or [{B}, {N}], got {tuple(pos.shape)}")
-    _call(q, lib().hla_rope, qv, kv, _rows(q_out, "q_out", q), kov, _ptr(pos), stride, _ptr(freqs), B,
-          heads, kv_heads, N, d, freqs.numel(), int(grid_w), int(interleaved), int(inverse),
-          float(magnitude), code)
+    _call(q, lib().hla_rope, qv, kv, qov, kov, _ptr(pos), stride, freqs.data_ptr(), B, heads, kv_heads,
+          N, d, freqs.numel(), int(grid_w), int(interleaved), int(inverse), float(magnitude), code)
     return q_out if k is None else (q_out, k_out)
 
 
@@ -792,7 +810,7 @@ def _cross_sizes(q, k, v, lengths):
                                             f"{tuple(k.shape)} and {tuple(v.shape)}")
     if lengths is not None:
         _require_on(lengths, "lengths", q, torch.int32)
-        if tuple(lengths.shape) != (B,):
+        if lengths.shape != (B,):
             raise HLAError(HLA_ERR_INVALID_ARG, f"lengths must be [{B}], got {tuple(lengths.shape)}")
     return views, (B, heads, kv, N, M, d), _dtype_code(q)
 
@@ -800,18 +818,8 @@ def _cross_sizes(q, k, v, lengths):
 def _cross_work(q, sizes, code, backward):
     """A workspace for one call (None where it needs none) and its bytes."""
     n = ctypes.c_int64()
-    with torch.cuda.device(q.device) if q.get_device() != torch.cuda.current_device() else nullcontext():
-        _check(lib().hla_cross_attn_workspace(*sizes, code, backward, ctypes.byref(n)))
+    _on_device_of(q, lib().hla_cross_attn_workspace, *sizes, code, backward, ctypes.byref(n))
     return (q.new_empty(n.value, dtype=torch.uint8) if n.value else None), n.value
-
-
-def _rows_like(t, name, like, shape):
-    """An output of a shape (default: a new tensor laid out as ``like``) and its view."""
-    if t is None:
-        t = torch.empty_like(like)
-    elif t.shape != shape:
-        raise HLAError(HLA_ERR_INVALID_ARG, f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    return t, _rows(t, name, like)
 
 
 def _lse_of(lse, q):
@@ -833,7 +841,7 @@ def cross_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     Tensors may be strided, rows contiguous: q from a token-wise projection is
     ``linear(x, w).view(B, N, heads, d).transpose(1, 2)``; out is laid out like q."""
     (qv, kv, vv), sizes, code = _cross_sizes(q, k, v, lengths)
-    out, ov = _rows_like(out, "out", q, q.shape)
+    out, ov = _rows_like(out, "out", q)
     if lse is not None:
         _lse_of(lse, q)
     elif with_lse:
@@ -857,9 +865,9 @@ def cross_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
         if not isinstance(t, torch.Tensor) or t.shape != q.shape:
             raise HLAError(HLA_ERR_INVALID_ARG, f"{name} must be {tuple(q.shape)}")
     _lse_of(lse, q)
-    dq, dqv = _rows_like(dq, "dq", q, q.shape)
-    dk, dkv = _rows_like(dk, "dk", k, k.shape)
-    dv, dvv = _rows_like(dv, "dv", v, v.shape)
+    dq, dqv = _rows_like(dq, "dq", q)
+    dk, dkv = _rows_like(dk, "dk", k)
+    dv, dvv = _rows_like(dv, "dv", v)
     work, n = _cross_work(q, sizes, code, 1)
     _call(q, lib().hla_cross_attn_bwd, qv, kv, vv, _rows(out, "out", q), _rows(dout, "dout", q), _ptr(lse),
           _ptr(lengths), dqv, dkv, dvv, *sizes, code,
@@ -898,8 +906,7 @@ def _shaped(t, name, like, shape):
 def _linear_work(x, T, K, F, act_code, code, backward):
     """A workspace for one call (None where it needs none) and its bytes."""
     n = ctypes.c_int64()
-    with torch.cuda.device(x.device) if x.get_device() != torch.cuda.current_device() else nullcontext():
-        _check(lib().hla_linear_workspace(T, K, F, act_code, code, backward, ctypes.byref(n)))
+    _on_device_of(x, lib().hla_linear_workspace, T, K, F, act_code, code, backward, ctypes.byref(n))
     return (x.new_empty(n.value, dtype=torch.uint8) if n.value else None), n.value
 
 

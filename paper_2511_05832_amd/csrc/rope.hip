@@ -4,27 +4,27 @@
 // with -a in place of a for the way back of a gradient; the other features are copied.
 //
 // Bound by HBM: each row is read and written once. A thread owns one unit of a row -
-// the 16-byte chunks that hold a run of pairs, or one chunk to copy - at one position,
-// computes the unit's sines and cosines once, and goes through a run of (batch, head)
-// slices with them, so the trigonometry (about 60 operations per pair) is shared. The
-// runs are as long as leaves the chip enough threads.
+// a run of pairs that 16 bytes hold, or as many to copy - at one position, computes the
+// unit's sines and cosines once, and goes through a run of (batch, head) slices with
+// them, so the trigonometry (about 60 operations per pair) is shared. The runs leave the
+// chip 32 waves per CU, two slices' loads in flight each. Measured: 64x64 layer, 6 heads
+// of 32, batch 16, bf16 18 us (5.6 TB/s); 65536 tokens, 8 + 2 heads of 64, fp32 57 us
+// (5.9 TB/s; a copy of 1 GiB 5.1).
+// Results go past the caches where a call moves more than they hold (256 MB): there
+// 77 -> 57 us, while at 84 MB 16.4 -> 18.4 and the next kernel finds its inputs in memory.
 //
 // The angle is formed in float64 and reduced to a fraction of a turn before it is
 // rounded: at position 10^5 and frequency 1 the float32 product is already 4e-3 off,
 // while this is below 2e-7 up to 2^28.
+#include <type_traits>
+
 #include "attn_common.h"
 
 namespace hla {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBatch = 4;   // slices whose loads are in flight together
-
-template <typename T>
-struct Chunk {
-  static constexpr int V = 16 / (int)sizeof(T);
-  typedef T type __attribute__((ext_vector_type(V)));
-};
+constexpr int kBatch = 2;   // slices whose loads are in flight together
 
 // cos and sin (times the magnitude, the sign of the direction included) of position
 // coordinate c and frequency f.
@@ -37,14 +37,16 @@ __device__ __forceinline__ void turn_of(double c, double f, const RopeArgs &p, f
   sn = s * (p.inverse ? -p.magnitude : p.magnitude);
 }
 
-// KIND 0: interleaved pairs, a unit is one chunk. KIND 1: halves whose length is a
-// multiple of a chunk, a unit is a chunk of the first half and its partner. KIND 2: any
-// other, a unit is one pair (or two features to copy), element by element.
-template <typename T, int KIND>
+// V: elements per access, the most that divide the run of pairs and fit 16 bytes (a
+// run of an odd number of pairs in halves: 1). INTER: interleaved pairs, a unit is one
+// access; else a unit of pairs is an access to the first half and its partner in the
+// second.
+template <typename T, int V, bool INTER, bool THROUGH>
 __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
-  constexpr int V = Chunk<T>::V;
-  typedef typename Chunk<T>::type vec;
-  constexpr int NP = KIND == 0 ? V / 2 : (KIND == 1 ? V : 1);   // pairs per unit
+  constexpr int VT = V == 1 ? 2 : V;      // elements of a unit to copy (their number is even)
+  typedef T vec __attribute__((ext_vector_type(V)));
+  typedef T tail __attribute__((ext_vector_type(VT)));
+  constexpr int NP = INTER ? V / 2 : V;   // pairs per unit
   const uint32_t idx = blockIdx.x * (uint32_t)kThreads + threadIdx.x;
   if (idx >= p.total) return;
   const uint32_t rows = fdiv(idx, p.unit_div);
@@ -68,27 +70,20 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
   }
   int h = s0 - b * HT;
 
-  // The unit's features (e0, and e1 for its partner) and its first pair.
+  // The unit's features (from e0 on, and from e1 on for the partners) and its first pair.
   const int P = p.pairs, rot = 2 * P * p.axes;
-  int e0, e1 = 0, pair, axis;
-  bool turned;
-  if constexpr (KIND == 0) {
-    e0 = u * V;
-    turned = e0 < rot;
-    pair = e0 / 2;
-    axis = 0;   // (per pair below: a chunk may cross from rows to columns)
-  } else {
-    const int per = KIND == 1 ? P / V : P;             // units per axis
-    const int nt = per * p.axes;
+  int e0 = u * V, e1 = 0, pair = e0 / 2, axis = 0;
+  bool turned = e0 < rot;
+  if constexpr (!INTER) {
+    const int per = P / V, nt = per * p.axes;   // units of pairs per axis, in all
     turned = u < nt;
-    axis = turned && u >= per ? 1 : 0;
-    pair = (u - axis * per) * (KIND == 1 ? V : 1);
     if (turned) {
-      e0 = KIND == 2 && p.interleaved ? 2 * (axis * P + pair) : axis * 2 * P + pair;
-      e1 = KIND == 2 && p.interleaved ? e0 + 1 : e0 + P;
+      axis = u >= per ? 1 : 0;
+      pair = (u - axis * per) * V;
+      e0 = axis * 2 * P + pair;
+      e1 = e0 + P;
     } else {
-      e0 = rot + (u - nt) * (KIND == 1 ? V : 2);
-      e1 = e0 + 1;
+      e0 = rot + (u - nt) * VT;
     }
   }
 
@@ -103,7 +98,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       int pi = pair + i, ax = axis;
-      if (KIND == 0 && pi >= P) {
+      if (INTER && pi >= P) {   // (a unit may cross from the row's pairs to the column's)
         pi -= P;
         ax = 1;
       }
@@ -129,67 +124,59 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
         ++b;
       }
     }
-    if constexpr (KIND == 2) {
+    auto put = [](T *q, const auto &v) {
+      using W = std::remove_const_t<std::remove_reference_t<decltype(v)>>;
+      if constexpr (THROUGH) __builtin_nontemporal_store(v, reinterpret_cast<W *>(q));
+      else *reinterpret_cast<W *>(q) = v;
+    };
+    if (!INTER && !turned) {
+      tail x[kBatch];
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        if (j >= m) break;
-        const T t0 = src[j][e0], t1 = src[j][e1];
-        const float x1 = (float)t0, x2 = (float)t1;
-        dst[j][e0] = turned ? (T)(x1 * cs[0] - x2 * sn[0]) : t0;
-        dst[j][e1] = turned ? (T)(x2 * cs[0] + x1 * sn[0]) : t1;
-      }
-    } else {
-      vec a[kBatch], c[kBatch];
+      for (int j = 0; j < kBatch; ++j)
+        if (j < m) x[j] = *reinterpret_cast<const tail *>(src[j] + e0);
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        if (j >= m) break;
-        a[j] = *reinterpret_cast<const vec *>(src[j] + e0);
-        if (KIND == 1 && turned) c[j] = *reinterpret_cast<const vec *>(src[j] + e1);
-      }
+      for (int j = 0; j < kBatch; ++j)
+        if (j < m) put(dst[j] + e0, x[j]);
+      continue;
+    }
+    vec a[kBatch], c[kBatch];
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        if (j >= m) break;
-        if (turned) {
+    for (int j = 0; j < kBatch; ++j) {
+      if (j >= m) break;
+      a[j] = *reinterpret_cast<const vec *>(src[j] + e0);
+      if (!INTER) c[j] = *reinterpret_cast<const vec *>(src[j] + e1);
+    }
 #pragma unroll
-          for (int i = 0; i < NP; ++i) {
-            if constexpr (KIND == 0) {
-              const float x1 = (float)a[j][2 * i], x2 = (float)a[j][2 * i + 1];
-              a[j][2 * i] = (T)(x1 * cs[i] - x2 * sn[i]);
-              a[j][2 * i + 1] = (T)(x2 * cs[i] + x1 * sn[i]);
-            } else {
-              const float x1 = (float)a[j][i], x2 = (float)c[j][i];
-              a[j][i] = (T)(x1 * cs[i] - x2 * sn[i]);
-              c[j][i] = (T)(x2 * cs[i] + x1 * sn[i]);
-            }
+    for (int j = 0; j < kBatch; ++j) {
+      if (j >= m) break;
+      if (!INTER || turned) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          if constexpr (INTER) {
+            const float x1 = (float)a[j][2 * i], x2 = (float)a[j][2 * i + 1];
+            a[j][2 * i] = (T)(x1 * cs[i] - x2 * sn[i]);
+            a[j][2 * i + 1] = (T)(x2 * cs[i] + x1 * sn[i]);
+          } else {
+            const float x1 = (float)a[j][i], x2 = (float)c[j][i];
+            a[j][i] = (T)(x1 * cs[i] - x2 * sn[i]);
+            c[j][i] = (T)(x2 * cs[i] + x1 * sn[i]);
           }
         }
-        *reinterpret_cast<vec *>(dst[j] + e0) = a[j];
-        if (KIND == 1 && turned) *reinterpret_cast<vec *>(dst[j] + e1) = c[j];
       }
+      put(dst[j] + e0, a[j]);
+      if (!INTER) put(dst[j] + e1, c[j]);
     }
   }
 }
 
-template <typename T>
+template <typename T, int V, bool INTER>
 hipError_t launch(RopeArgs &p, hipStream_t s) {
-  constexpr int V = Chunk<T>::V;
   const int rot = 2 * p.pairs * p.axes;
-  int kind, units;
-  if (p.interleaved && rot % V == 0) {
-    kind = 0;
-    units = p.d / V;
-  } else if (!p.interleaved && p.pairs % V == 0) {
-    kind = 1;
-    units = rot / (2 * V) + (p.d - rot) / V;
-  } else {
-    kind = 2;
-    units = p.d / 2;
-  }
+  const int units = INTER ? p.d / V : rot / (2 * V) + (p.d - rot) / (V == 1 ? 2 : V);
   p.unit_div = make_fastdiv((uint32_t)units);
   p.n_div = make_fastdiv((uint32_t)p.N);
-  // Runs of slices as long as leaves every CU eight waves of threads.
   const int64_t per_slice = (int64_t)units * p.N, HT = p.heads[0] + p.heads[1];
-  const int64_t want = (int64_t)device_cu_count() * 512;
+  const int64_t want = (int64_t)device_cu_count() * 2048;
   int64_t run = per_slice * HT * p.B / want;
   const int64_t most = p.pos_stride ? HT : HT * p.B;
   run = run < 1 ? 1 : (run > most ? most : run);
@@ -198,16 +185,33 @@ hipError_t launch(RopeArgs &p, hipStream_t s) {
   const int64_t total = per_slice * p.groups * (p.pos_stride ? p.B : 1);
   p.total = (uint32_t)total;
   const dim3 grid((uint32_t)((total + kThreads - 1) / kThreads));
-  if (kind == 0) hipLaunchKernelGGL((rope_kernel<T, 0>), grid, dim3(kThreads), 0, s, p);
-  else if (kind == 1) hipLaunchKernelGGL((rope_kernel<T, 1>), grid, dim3(kThreads), 0, s, p);
-  else hipLaunchKernelGGL((rope_kernel<T, 2>), grid, dim3(kThreads), 0, s, p);
+  const int64_t bytes = 2 * p.B * HT * p.N * p.d * (int64_t)sizeof(T);
+  if (bytes > (256LL << 20)) hipLaunchKernelGGL((rope_kernel<T, V, INTER, true>), grid, dim3(kThreads), 0, s, p);
+  else hipLaunchKernelGGL((rope_kernel<T, V, INTER, false>), grid, dim3(kThreads), 0, s, p);
   return hipGetLastError();
+}
+
+// The widest access that divides the features of an axis' pairs (interleaved) or the
+// pairs themselves.
+template <typename T>
+hipError_t launch_any(RopeArgs &p, hipStream_t s) {
+  constexpr int V = 16 / (int)sizeof(T);
+  if (p.interleaved) {
+    const int n = 2 * p.pairs * p.axes;
+    if (n % V == 0) return launch<T, V, true>(p, s);
+    if (V == 8 && n % 4 == 0) return launch<T, 4, true>(p, s);
+    return launch<T, 2, true>(p, s);
+  }
+  if (p.pairs % V == 0) return launch<T, V, false>(p, s);
+  if (V == 8 && p.pairs % 4 == 0) return launch<T, 4, false>(p, s);
+  if (p.pairs % 2 == 0) return launch<T, 2, false>(p, s);
+  return launch<T, 1, false>(p, s);
 }
 
 }  // namespace
 
 hipError_t launch_rope(RopeArgs p, hla_dtype dtype, hipStream_t s) {
-  return dtype == HLA_BF16 ? launch<__bf16>(p, s) : launch<float>(p, s);
+  return dtype == HLA_BF16 ? launch_any<__bf16>(p, s) : launch_any<float>(p, s);
 }
 
 }  // namespace hla
