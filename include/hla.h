@@ -503,8 +503,9 @@ hla_status hla_rope(const hla_view *q, const hla_view *k, const hla_view *q_out,
  * these sizes on the current device, 16-byte aligned, overlapping no tensor; may be
  * NULL where that is 0. A call's work is done with it when the call's work is done;
  * calls whose work overlaps in time need one each.
- * Supported: d in {32, 64}; row strides of k and v below 2^25 bytes; heads / kv_heads
- * * N below 2^30; otherwise UNSUPPORTED.
+ * Supported: d in {32, 64}; row strides of k and v below 2^25 bytes; a batch element of a
+ * view within 2^36 bytes; M, heads / kv_heads * N and B * kv_heads up to 2^30, and that
+ * times either list of rows up to 2^36; otherwise UNSUPPORTED.
  */
 hla_status hla_cross_attn_fwd(const hla_view *q, const hla_view *k, const hla_view *v,
                               const int32_t *lengths, const hla_view *out, float *lse, int64_t B,

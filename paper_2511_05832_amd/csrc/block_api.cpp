@@ -151,7 +151,9 @@ hla_status hla_rope(const hla_view *q, const hla_view *k, const hla_view *q_out,
 
 namespace {
 
-CrossStride cross_stride(const ViewShape &s) { return {s.v.batch, s.v.head, s.v.row}; }
+CrossStride cross_stride(const ViewShape &s) {
+  return {s.v.batch * s.es, (uint32_t)(s.v.head * s.es / 16), (uint32_t)(s.v.row * s.es / 16)};
+}
 
 // Sizes of a cross attention, into the kernel's arguments, and its workspace.
 hla_status cross_sizes(int64_t B, int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d,
@@ -178,7 +180,8 @@ hla_status cross_sizes(int64_t B, int64_t heads, int64_t kv_heads, int64_t N, in
   a->R = (int32_t)R;
   a->Rp = (int32_t)((R + 127) / 128 * 128);
   a->ndiv = make_fastdiv((uint32_t)N);
-  const bool parts = backward ? cross_bwd_plan(*a) : cross_fwd_plan(*a);
+  const int row_bytes = (int)(d * dtype_size(dtype));
+  const bool parts = backward ? cross_bwd_plan(*a, row_bytes) : cross_fwd_plan(*a, row_bytes);
   *bytes = backward ? 8 * bk * a->Rp + (parts ? bk * a->splits * M * 8 * d : 0)
                     : (parts ? bk * a->splits * R * (4 * d + 8) : 0);
   return HLA_OK;
@@ -211,6 +214,9 @@ hla_status cross_views(ViewShape *t, int n_in, int n, std::initializer_list<Rang
   hla_status st;
   for (int i = 0; i < n; ++i)
     if ((st = check_view(t[i], i >= n_in)) != HLA_OK) return st;
+  for (int i = 0; i < n; ++i)
+    if (((t[i].size[1] - 1) * t[i].v.head + (t[i].size[2] - 1) * t[i].v.row) * t[i].es >= (1LL << 36))
+      return fail(HLA_ERR_UNSUPPORTED, "a batch element of %s reaches over 2^36 bytes", t[i].name);
   for (int i = 1; i < 3; ++i)   // k, v
     if (t[i].v.row * t[i].es >= (1 << 25))
       return fail(HLA_ERR_UNSUPPORTED, "the rows of %s must lie less than 2^25 bytes apart", t[i].name);

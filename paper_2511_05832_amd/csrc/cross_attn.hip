@@ -43,16 +43,24 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 }
 __device__ __forceinline__ float inv_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
+// Row r of key head kvh: query n of a head.
 struct Row {
-  int head, n;
+  uint32_t head, n;
 };
 __device__ __forceinline__ Row row_of(const CrossArgs &a, int r, int kvh) {
-  const int g = (int)fdiv((uint32_t)r, a.ndiv);
+  if (a.G == 1) return {(uint32_t)kvh, (uint32_t)r};
+  const uint32_t g = fdiv((uint32_t)r, a.ndiv);
   return {kvh * a.G + g, r - g * a.N};
 }
+// Its address: 32-bit arithmetic in units of 16 bytes within the batch element.
 template <typename T>
 __device__ __forceinline__ T *row_ptr(const void *p, const CrossStride &s, int b, const Row &r) {
-  return const_cast<T *>(static_cast<const T *>(p)) + b * s.batch + r.head * s.head + r.n * s.row;
+  char *base = static_cast<char *>(const_cast<void *>(p)) + b * s.batch;
+  return reinterpret_cast<T *>(base + ((uint64_t)(r.head * s.head + r.n * s.row) << 4));
+}
+// The first row of key head kvh.
+__device__ __forceinline__ const char *head_ptr(const void *p, const CrossStride &s, int b, int kvh) {
+  return static_cast<const char *>(p) + b * s.batch + ((uint64_t)(kvh * s.head) << 4);
 }
 
 // Workgroup -> piece of work. The pieces are ordered by (batch, key head), whose keys they
@@ -119,8 +127,9 @@ struct Softmax {
     primed = false;
     fresh = true;
   }
-  // weights of NB blocks in place of their scores; returns the new sum
-  template <int NB>
+  // weights of NB blocks in place of their scores; returns the new sum. NV = 8: only
+  // the first 16 keys are seen (a lane's first eight slots).
+  template <int NB, int NV = 16>
   __device__ __forceinline__ float weights(f32x16 (&s)[NB], float scale, float ref) const {
     float sum[NB];
 #pragma unroll
@@ -129,6 +138,10 @@ struct Softmax {
     for (int v = 0; v < 16; ++v)
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
+        if (v >= NV) {
+          s[b][v] = 0.f;
+          continue;
+        }
         s[b][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][v], scale, -ref));
         sum[b] += s[b][v];
       }
@@ -156,7 +169,7 @@ struct Softmax {
     float ln = 0.f;
     bool slow = !primed;
     if (primed || fresh) {
-      ln = weights(s, scale, fresh ? 0.f : m);
+      ln = TAIL && left <= 16 ? weights<NB, 8>(s, scale, fresh ? 0.f : m) : weights(s, scale, fresh ? 0.f : m);
       const bool bad = !(ln <= 4294967296.f) || (fresh && !(ln >= 1.f / 4294967296.f));
       slow = false;
       if (!__ballot(bad)) {
@@ -225,9 +238,8 @@ __global__ void __launch_bounds__(256, 2) cross_fwd(CrossArgs a) {
   if (logical >= a.total) return;
   const int rt = logical % a.n_rtiles, bk = logical / a.n_rtiles, b = bk / a.kv, kvh = bk - b * a.kv;
   const int len = keys_of(a, b), nt = (len + BN - 1) / BN;
-  const char *K = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head);
-  const char *V = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + b * a.vs.batch + kvh * a.vs.head);
-  const uint32_t kr = (uint32_t)a.ks.row * sizeof(T), vr = (uint32_t)a.vs.row * sizeof(T);
+  const char *K = head_ptr(a.k, a.ks, b, kvh), *V = head_ptr(a.v, a.vs, b, kvh);
+  const uint32_t kr = a.ks.row * 16, vr = a.vs.row * 16;
   auto issue = [&](int i) {
     const int at = i * BN;
     Copy::issue(K + (int64_t)at * kr, V + (int64_t)at * vr, kr, vr, len - 1 - at, lds + (i % RING) * STAGE, wave, lane);
@@ -288,10 +300,10 @@ struct FewRows {
     k1 = min(k0 + a.per, len);
     const int tiles = k1 > k0 ? (k1 - k0 + BN - 1) / BN : 0;
     nt = (tiles - wave + 3) / 4;
-    K = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head);
-    V = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + b * a.vs.batch + kvh * a.vs.head);
-    kr = (uint32_t)a.ks.row * sizeof(T);
-    vr = (uint32_t)a.vs.row * sizeof(T);
+    K = head_ptr(a.k, a.ks, b, kvh);
+    V = head_ptr(a.v, a.vs, b, kvh);
+    kr = a.ks.row * 16;
+    vr = a.vs.row * 16;
     ring = lds + wave * RING * STAGE;
   }
   __device__ __forceinline__ int first(int i, int wave) const { return k0 + (4 * i + wave) * BN; }
@@ -403,8 +415,9 @@ __global__ void __launch_bounds__(256, 1) cross_fwd_few(CrossArgs a) {
 // Up to 128 keys (a text's tokens): keys and values stay in LDS, and a workgroup's waves,
 // each for itself, go through blocks of 32 rows with the next block's queries in flight.
 // Bound by HBM (q in, out out). (16 x 6 heads of 32, 4096 rows against 77 keys.)
-// (fp32 rows of 64: 98 KiB of LDS leave one workgroup per CU)
-constexpr int short_waves(int row_bytes) { return row_bytes > 128 ? 1 : 2; }
+// Workgroups per CU of the kernels whose keys stay in LDS: what their registers (three,
+// two for rows of 128 bytes) or LDS (fp32 rows of 64: 98 KiB, one) leave.
+constexpr int short_waves(int row_bytes) { return row_bytes > 128 ? 1 : (row_bytes > 64 ? 2 : 3); }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256, short_waves(sizeof(T) * D)) cross_fwd_short(CrossArgs a) {
@@ -417,9 +430,8 @@ __global__ void __launch_bounds__(256, short_waves(sizeof(T) * D)) cross_fwd_sho
   if (logical >= a.total) return;
   const int part = logical % a.row_parts, bk = logical / a.row_parts, b = bk / a.kv, kvh = bk - b * a.kv;
   const int len = keys_of(a, b), nt = (len + BN - 1) / BN;
-  const char *K = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head);
-  const char *V = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + b * a.vs.batch + kvh * a.vs.head);
-  const uint32_t kr = (uint32_t)a.ks.row * sizeof(T), vr = (uint32_t)a.vs.row * sizeof(T);
+  const char *K = head_ptr(a.k, a.ks, b, kvh), *V = head_ptr(a.v, a.vs, b, kvh);
+  const uint32_t kr = a.ks.row * 16, vr = a.vs.row * 16;
   for (int i = 0; i < nt; ++i)
     KvCopy<T, D, 4>::issue(K + (int64_t)i * BN * kr, V + (int64_t)i * BN * vr, kr, vr, len - 1 - i * BN, lds + i * STAGE, wave, lane);
   const int nblk = (a.R + 31) / 32, step = 4 * a.row_parts;
@@ -556,9 +568,8 @@ __global__ void __launch_bounds__(256, 2) cross_dq(CrossArgs a) {
   if (logical >= a.total) return;
   const int rt = logical % a.n_rtiles, bk = logical / a.n_rtiles, b = bk / a.kv, kvh = bk - b * a.kv;
   const int len = keys_of(a, b), nt = (len + BN - 1) / BN;
-  const char *K = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head);
-  const char *V = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + b * a.vs.batch + kvh * a.vs.head);
-  const uint32_t kr = (uint32_t)a.ks.row * sizeof(T), vr = (uint32_t)a.vs.row * sizeof(T);
+  const char *K = head_ptr(a.k, a.ks, b, kvh), *V = head_ptr(a.v, a.vs, b, kvh);
+  const uint32_t kr = a.ks.row * 16, vr = a.vs.row * 16;
   auto issue = [&](int i) {
     const int at = i * BN;
     Copy::issue(K + (int64_t)at * kr, V + (int64_t)at * vr, kr, vr, len - 1 - at, lds + (i % RING) * STAGE, wave, lane);
@@ -646,9 +657,8 @@ __global__ void __launch_bounds__(256, short_waves(sizeof(T) * D)) cross_dq_shor
   if (logical >= a.total) return;
   const int part = logical % a.row_parts, bk = logical / a.row_parts, b = bk / a.kv, kvh = bk - b * a.kv;
   const int len = keys_of(a, b), nt = (len + BN - 1) / BN;
-  const char *K = reinterpret_cast<const char *>(static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head);
-  const char *V = reinterpret_cast<const char *>(static_cast<const T *>(a.v) + b * a.vs.batch + kvh * a.vs.head);
-  const uint32_t kr = (uint32_t)a.ks.row * sizeof(T), vr = (uint32_t)a.vs.row * sizeof(T);
+  const char *K = head_ptr(a.k, a.ks, b, kvh), *V = head_ptr(a.v, a.vs, b, kvh);
+  const uint32_t kr = a.ks.row * 16, vr = a.vs.row * 16;
   for (int i = 0; i < nt; ++i)
     KvCopy<T, D, 4>::issue(K + (int64_t)i * BN * kr, V + (int64_t)i * BN * vr, kr, vr, len - 1 - i * BN, lds + i * STAGE, wave, lane);
   // (blocks up to the padded end of the list: their statistics are read by the next kernel)
@@ -732,10 +742,10 @@ __global__ void __launch_bounds__(64 * KB * RH, 2) cross_dkdv(CrossArgs a) {
   for (int i = 0; i < RING - 1; ++i)
     if (i0 + i < i1) issue(i0 + i);
 
-  const int64_t krow = min(kpos, max(len - 1, 0));   // (unseen keys: not stored)
+  const Row krow = {(uint32_t)kvh, (uint32_t)min(kpos, max(len - 1, 0))};   // (unseen keys: not stored)
   typename Tl::Frag k, v;
-  Tl::load(k, static_cast<const T *>(a.k) + b * a.ks.batch + kvh * a.ks.head + krow * a.ks.row, half);
-  Tl::load(v, static_cast<const T *>(a.v) + b * a.vs.batch + kvh * a.vs.head + krow * a.vs.row, half);
+  Tl::load(k, row_ptr<T>(a.k, a.ks, b, krow), half);
+  Tl::load(v, row_ptr<T>(a.v, a.vs, b, krow), half);
   Tl tl;
   tl.init(lane);
   f32x16 dk[NDB], dv[NDB];
@@ -802,9 +812,9 @@ __global__ void __launch_bounds__(64 * KB * RH, 2) cross_dkdv(CrossArgs a) {
       for (int db = 0; db < NDB; ++db) sum[db] = f32x16{};
     }
     const CrossStride &os = which ? a.dvs : a.dks;
-    T *dst = static_cast<T *>(which ? a.dv : a.dk) + b * os.batch + kvh * os.head;
-    store_rows<T, D>(lds + wave * AREA, sum, which ? 1.f : a.scale, lane,
-                     [&](int i) { return j0 + i < a.M ? dst + (j0 + i) * os.row : nullptr; });
+    store_rows<T, D>(lds + wave * AREA, sum, which ? 1.f : a.scale, lane, [&](int i) {
+      return j0 + i < a.M ? row_ptr<T>(which ? a.dv : a.dk, os, b, {(uint32_t)kvh, (uint32_t)(j0 + i)}) : nullptr;
+    });
   };
   put(dk, RH == 2 ? rh : 0);
   if constexpr (RH == 1) put(dv, 1);
@@ -825,7 +835,7 @@ __global__ void __launch_bounds__(256) cross_sum(CrossArgs a) {
     for (int s = 0; s < a.splits; ++s) sum += *reinterpret_cast<const f32x4 *>(p + s * keys * 2 * D);
   }
   const CrossStride &os = which ? a.dvs : a.dks;
-  T *dst = static_cast<T *>(which ? a.dv : a.dk) + b * os.batch + kvh * os.head + j * os.row;
+  T *dst = row_ptr<T>(which ? a.dv : a.dk, os, b, {(uint32_t)kvh, (uint32_t)j});
   put4<T>(dst + c, sum * (which ? 1.f : a.scale));
 }
 
@@ -906,18 +916,21 @@ int up_to(int64_t want, int64_t most) { return (int)std::max<int64_t>(1, std::mi
 
 }  // namespace
 
-// How the rows are shared out where the keys stay in LDS: four workgroups per CU, a block
-// of rows or more for each wave.
-static void share_rows(CrossArgs &a) {
-  a.row_parts = up_to(4 * (int64_t)device_cu_count() / ((int64_t)a.B * a.kv), (a.R + 127) / 128);
+// How the rows are shared out where the keys stay in LDS: as many blocks to a wave as let
+// all workgroups run at once.
+static void share_rows(CrossArgs &a, int row_bytes) {
+  const int64_t slots = (int64_t)device_cu_count() * short_waves(row_bytes), bk = (int64_t)a.B * a.kv;
+  const int64_t parts = up_to(slots / bk, (a.R + 127) / 128), blocks = (a.R + 31) / 32;
+  const int64_t each = (blocks + 4 * parts - 1) / (4 * parts);
+  a.row_parts = (int)((blocks + 4 * each - 1) / (4 * each));
 }
 
 // Key splits of the forward: one workgroup per CU (its LDS is full), of at least eight
 // tiles each.
-bool cross_fwd_plan(CrossArgs &a) {
+bool cross_fwd_plan(CrossArgs &a, int row_bytes) {
   a.splits = 1;
   a.per = (a.M + BN - 1) / BN * BN;
-  share_rows(a);
+  share_rows(a, row_bytes);
   if (keys_stay(a) || !few_rows(a)) return false;
   const int64_t wgs = (int64_t)a.B * a.kv * ((a.R + 31) / 32), tiles = (a.M + BN - 1) / BN;
   const int splits = up_to(device_cu_count() / wgs, (tiles + 7) / 8);
@@ -927,10 +940,10 @@ bool cross_fwd_plan(CrossArgs &a) {
 }
 
 // Row splits of dk and dv: eight waves per CU, at least 128 rows each.
-bool cross_bwd_plan(CrossArgs &a) {
+bool cross_bwd_plan(CrossArgs &a, int row_bytes) {
   a.splits = 1;
   a.per = (a.M + BN - 1) / BN * BN;
-  share_rows(a);
+  share_rows(a, row_bytes);
   const int kb = kv_blocks(a);
   a.n_ktiles = (a.M + 32 * kb - 1) / (32 * kb);
   a.splits = up_to((int64_t)device_cu_count() * (kb == 2 ? 2 : 1) / ((int64_t)a.B * a.kv * a.n_ktiles), (a.R + 127) / 128);

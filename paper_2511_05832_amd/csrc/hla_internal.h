@@ -192,9 +192,11 @@ struct RopeArgs {
 hipError_t launch_rope(RopeArgs a, hla_dtype dtype, hipStream_t s);
 
 // Cross attention. Row r of a (batch, key head) pair is query r % N of head
-// kvh * G + r / N. Strides in elements.
+// kvh * G + r / N. Strides: batch in bytes; head and row in units of 16 bytes, within a
+// batch element 32 bits.
 struct CrossStride {
-  int64_t batch, head, row;
+  int64_t batch;
+  uint32_t head, row;
 };
 struct CrossArgs {
   const void *q, *k, *v, *dout;
@@ -214,8 +216,8 @@ struct CrossArgs {
   float scale, scale_log2;
 };
 // Share out the work, from B, kv, R and M; true: partial sums go to a workspace.
-bool cross_fwd_plan(CrossArgs &a);
-bool cross_bwd_plan(CrossArgs &a);
+bool cross_fwd_plan(CrossArgs &a, int row_bytes);
+bool cross_bwd_plan(CrossArgs &a, int row_bytes);
 hipError_t launch_cross_fwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s);
 hipError_t launch_cross_bwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s);
 

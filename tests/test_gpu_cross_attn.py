@@ -330,6 +330,7 @@ ROW = (64 * 64 * 4, 64 * 64, 64)
     (dict(k=(Raw.K, *ROW[:2], 60)), INV, "stride"),
     (dict(v=(Raw.V, *ROW[:2], -64)), INV, "stride"),
     (dict(k=(Raw.K, *ROW[:2], 1 << 24)), UNS, "2^25"),
+    (dict(q=(Raw.Q, 1 << 45, 1 << 36, 64)), UNS, "2^36"),
     (dict(work=0, M=100000, N=64, B=1, heads=1, kv=1), INV, "work"),
     (dict(lse=Raw.W, N=1, M=4096, B=1, heads=1, kv=1), INV, "overlaps"),
 ], ids=str)
