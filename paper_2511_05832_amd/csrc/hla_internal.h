@@ -231,7 +231,7 @@ struct LinearArgs {
 };
 // Byte offsets of the backward's workspace, and its size.
 struct LinearWork {
-  int64_t dz, part, sums, bytes;
+  int64_t dz, dx, dw, sums, bytes;
 };
 LinearWork linear_bwd_work(const LinearArgs &a, hla_dtype dtype);
 int64_t linear_fwd_work(const LinearArgs &a, hla_dtype dtype);

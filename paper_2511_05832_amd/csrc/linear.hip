@@ -315,9 +315,12 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) gemm_kernel(GemmArgs p) {
 }
 
 // The layer for few tokens (T <= 16 NB). What bounds it: reading W once. A workgroup
-// takes 16 features, its NW waves share the contraction in runs of 128 bytes a row;
-// rows of W go from memory into operands of the 16 x 16 products (A = features, B =
-// tokens), 1 KiB per load, with no stop in LDS. The waves' sums are added through LDS.
+// takes 16 features, its waves share the contraction in runs of 128 bytes a row; rows
+// of W go from memory into operands of the 16 x 16 products (A = features, B = tokens),
+// 1 KiB per load, with no stop in LDS. The waves' sums are added through LDS. 4 tokens,
+// 2048 -> 8192, bf16, weights from memory: 10.2 us (3.3 TB/s); with 4 waves and the same
+// loads in flight per wave 12.6, with 16 waves 12.0.
+constexpr int kFewWaves = 8;
 template <typename T>
 struct Few;
 template <>
@@ -334,9 +337,9 @@ struct Few<float> {
   }
 };
 
-template <typename T, int NB, int NW>
-__global__ void __launch_bounds__(64 * NW) few_kernel(GemmArgs p) {
-  constexpr int V = Type<T>::V, RUN = 128 / (int)sizeof(T), UNROLL = NB == 1 ? 4 : 2;
+template <typename T, int NB>
+__global__ void __launch_bounds__(64 * kFewWaves) few_kernel(GemmArgs p) {
+  constexpr int NW = kFewWaves, V = Type<T>::V, RUN = 128 / (int)sizeof(T), UNROLL = NB == 1 ? 4 : 2;
   typedef typename Type<T>::Op Op;
   __shared__ __attribute__((aligned(16))) f32x4 sums[NW][NB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -453,22 +456,41 @@ __global__ void __launch_bounds__(256) dz_kernel(const T *dy, const T *pre, T *d
   }
 }
 
-// out[i] = sum over n partial sums of part[s * len + i], four values per thread.
+// out[i] = sum over n partial sums of part[s * len + i], four values per thread, for up
+// to three results in one launch (a launch takes 3 to 5 us by itself).
+struct SumJob {
+  const float *part;
+  void *out;
+  int64_t len;
+  int32_t n, blocks;   // blocks = 0: nothing to do
+};
+struct SumJobs {
+  SumJob job[3];
+};
+
 template <typename T>
-__global__ void __launch_bounds__(256) sum_kernel(const float *part, T *out, int64_t len, int n) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (i >= len) return;
+__global__ void __launch_bounds__(256) sum_kernel(SumJobs jobs) {
+  int block = blockIdx.x, j = 0;
+  while (j < 2 && block >= jobs.job[j].blocks) block -= jobs.job[j++].blocks;
+  const SumJob &w = jobs.job[j];
+  const int64_t i = ((int64_t)block * 256 + threadIdx.x) * 4;
+  if (i >= w.len) return;
   f32x4 s = {};
-#pragma unroll 4
-  for (int k = 0; k < n; ++k) s += *reinterpret_cast<const f32x4 *>(part + k * len + i);
+#pragma unroll 8
+  for (int k = 0; k < w.n; ++k) s += *reinterpret_cast<const f32x4 *>(w.part + k * w.len + i);
+  T *out = static_cast<T *>(w.out) + i;
   if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<f32x4 *>(out + i) = s;
+    *reinterpret_cast<f32x4 *>(out) = s;
   } else {
     bf16x4 o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = (__bf16)s[e];
-    *reinterpret_cast<bf16x4 *>(out + i) = o;
+    *reinterpret_cast<bf16x4 *>(out) = o;
   }
+}
+
+SumJob sum_job(const float *part, void *out, int64_t len, int n) {
+  return {part, out, len, n, (int32_t)((len / 4 + 255) / 256)};
 }
 
 // The layer's epilogue over partial sums of its products: V columns of a row per thread.
@@ -526,7 +548,7 @@ Plan plan_of(int64_t NA, int64_t NB, int64_t KC, bool layer, bool parts) {
     p.splits = (int)((stages + p.stages - 1) / p.stages);
     return p;
   };
-  if (sizeof(T) == 4) return make(64, 128, 4 * cus, 4);
+  if (sizeof(T) == 4) return make(64, 128, 2 * cus, 4);
   const int64_t n256 = tiles(256), n128 = tiles(128);
   const bool fills = n256 * 5 >= (n256 + cus - 1) / cus * cus * 4;   // four fifths of its rounds
   if (KC >= 512 && fills) return make(256, 128, cus, 4);
@@ -560,16 +582,12 @@ hipError_t launch_gemm(GemmArgs &p, const Plan &plan, hipStream_t s) {
   return hipGetLastError();
 }
 
-// A product whose result is rounded to T: in one launch, or in parts and their sum.
+// A product whose result is rounded to T: in one launch, or in parts that `job` adds.
 template <typename T, bool AT, bool BT>
-hipError_t product(GemmArgs &p, const Plan &plan, hipStream_t s) {
+hipError_t product(GemmArgs &p, const Plan &plan, SumJob *job, hipStream_t s) {
   if (plan.splits == 1) return launch_gemm<T, AT, BT, EPI_PLAIN>(p, plan, s);
-  hipError_t e = launch_gemm<T, AT, BT, EPI_PART>(p, plan, s);
-  if (e != hipSuccess) return e;
-  const int64_t len = (int64_t)p.NB * p.NA;
-  hipLaunchKernelGGL((sum_kernel<T>), dim3((uint32_t)((len / 4 + 255) / 256)), dim3(256), 0, s, p.part,
-                     static_cast<T *>(p.out), len, plan.splits);
-  return hipGetLastError();
+  *job = sum_job(p.part, p.out, (int64_t)p.NB * p.NA, plan.splits);
+  return launch_gemm<T, AT, BT, EPI_PART>(p, plan, s);
 }
 
 constexpr int kFewTokens = 64;
@@ -593,15 +611,9 @@ hipError_t fwd(const LinearArgs &a, hipStream_t s) {
   p.act = a.act;
   if (a.T <= kFewTokens) {
     const dim3 grid((uint32_t)((a.F + 15) / 16));
-    // (more waves to a workgroup where there are few workgroups)
-    const bool wide = (int)grid.x >= device_cu_count();
-    if (a.T <= 16) {
-      if (wide) hipLaunchKernelGGL((few_kernel<T, 1, 4>), grid, dim3(256), 0, s, p);
-      else hipLaunchKernelGGL((few_kernel<T, 1, 16>), grid, dim3(1024), 0, s, p);
-    } else {
-      if (wide) hipLaunchKernelGGL((few_kernel<T, 4, 4>), grid, dim3(256), 0, s, p);
-      else hipLaunchKernelGGL((few_kernel<T, 4, 8>), grid, dim3(512), 0, s, p);
-    }
+    if (a.T <= 16) hipLaunchKernelGGL((few_kernel<T, 1>), grid, dim3(64 * kFewWaves), 0, s, p);
+    else if (a.T <= 32) hipLaunchKernelGGL((few_kernel<T, 2>), grid, dim3(64 * kFewWaves), 0, s, p);
+    else hipLaunchKernelGGL((few_kernel<T, 4>), grid, dim3(64 * kFewWaves), 0, s, p);
     return hipGetLastError();
   }
   const Plan plan = layer_plan<T>(a);
@@ -627,8 +639,9 @@ hipError_t bwd(const LinearArgs &a, hipStream_t s) {
   const LinearWork w = linear_bwd_work(a, sizeof(T) == 2 ? HLA_BF16 : HLA_F32);
   char *work = static_cast<char *>(a.work);
   T *dz = reinterpret_cast<T *>(work + w.dz);
-  float *part = reinterpret_cast<float *>(work + w.part), *sums = reinterpret_cast<float *>(work + w.sums);
+  float *sums = reinterpret_cast<float *>(work + w.sums);
   const bool has_act = a.act != HLA_ACT_NONE;
+  SumJobs jobs = {};   // dx, dW, db
   hipError_t e;
   if (has_act || a.db) {
     const int rows = dz_rows(a, V);
@@ -636,11 +649,7 @@ hipError_t bwd(const LinearArgs &a, hipStream_t s) {
     hipLaunchKernelGGL((dz_kernel<T>), grid, dim3(256), 0, s, static_cast<const T *>(a.dy), static_cast<const T *>(a.pre),
                        has_act ? dz : nullptr, a.db ? sums : nullptr, a.T, a.F, rows, a.act);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (a.db) {
-      hipLaunchKernelGGL((sum_kernel<T>), dim3((uint32_t)((a.F / 4 + 255) / 256)), dim3(256), 0, s, sums,
-                         static_cast<T *>(a.db), (int64_t)a.F, (int)grid.y);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
+    if (a.db) jobs.job[2] = sum_job(sums, a.db, a.F, (int)grid.y);
   }
   const void *g = has_act ? static_cast<const void *>(dz) : a.dy;
   if (a.dx) {
@@ -653,8 +662,8 @@ hipError_t bwd(const LinearArgs &a, hipStream_t s) {
     p.NB = a.T;
     p.KC = a.F;
     p.out = a.dx;
-    p.part = part;
-    if ((e = product<T, true, false>(p, plan_of<T>(a.K, a.T, a.F, false, true), s)) != hipSuccess) return e;
+    p.part = reinterpret_cast<float *>(work + w.dx);
+    if ((e = product<T, true, false>(p, plan_of<T>(a.K, a.T, a.F, false, true), &jobs.job[0], s)) != hipSuccess) return e;
   }
   if (a.dw) {
     GemmArgs p = {};
@@ -666,10 +675,13 @@ hipError_t bwd(const LinearArgs &a, hipStream_t s) {
     p.NB = a.F;
     p.KC = a.T;
     p.out = a.dw;
-    p.part = part;
-    if ((e = product<T, true, true>(p, plan_of<T>(a.K, a.F, a.T, false, true), s)) != hipSuccess) return e;
+    p.part = reinterpret_cast<float *>(work + w.dw);
+    if ((e = product<T, true, true>(p, plan_of<T>(a.K, a.F, a.T, false, true), &jobs.job[1], s)) != hipSuccess) return e;
   }
-  return hipSuccess;
+  const int64_t blocks = (int64_t)jobs.job[0].blocks + jobs.job[1].blocks + jobs.job[2].blocks;
+  if (!blocks) return hipSuccess;
+  hipLaunchKernelGGL((sum_kernel<T>), dim3((uint32_t)blocks), dim3(256), 0, s, jobs);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -682,10 +694,9 @@ LinearWork work_of(const LinearArgs &a) {
   auto parts = [&](const Plan &p, int64_t len) { return p.splits == 1 ? 0 : (int64_t)p.splits * len * 4; };
   LinearWork w;
   w.dz = 0;
-  w.part = a.act != HLA_ACT_NONE ? up((int64_t)a.T * a.F * sizeof(T)) : 0;
-  const int64_t dx = a.dx ? parts(plan_of<T>(a.K, a.T, a.F, false, true), (int64_t)a.T * a.K) : 0;
-  const int64_t dw = a.dw ? parts(plan_of<T>(a.K, a.F, a.T, false, true), (int64_t)a.F * a.K) : 0;
-  w.sums = w.part + up(std::max(dx, dw));
+  w.dx = a.act != HLA_ACT_NONE ? up((int64_t)a.T * a.F * sizeof(T)) : 0;
+  w.dw = w.dx + (a.dx ? up(parts(plan_of<T>(a.K, a.T, a.F, false, true), (int64_t)a.T * a.K)) : 0);
+  w.sums = w.dw + (a.dw ? up(parts(plan_of<T>(a.K, a.F, a.T, false, true), (int64_t)a.F * a.K)) : 0);
   const int rows = dz_rows(a, Type<T>::V);
   w.bytes = w.sums + (a.db ? up((int64_t)((a.T + rows - 1) / rows) * a.F * 4) : 0);
   return w;
@@ -700,8 +711,7 @@ int64_t layer_work(const LinearArgs &a) {
 
 }  // namespace
 
-// Workspace of the backward: dz, the products' partial sums (dx's and dW's in turn),
-// the bias' partial sums.
+// Workspace of the backward: dz, the partial sums of dx, dW and db.
 LinearWork linear_bwd_work(const LinearArgs &a, hla_dtype dtype) {
   return dtype == HLA_BF16 ? work_of<__bf16>(a) : work_of<float>(a);
 }
