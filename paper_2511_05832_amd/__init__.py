@@ -33,6 +33,7 @@ import ctypes
 import math
 import os
 import threading
+from functools import lru_cache
 from typing import Optional, Tuple
 
 import torch
@@ -815,11 +816,20 @@ def _cross_sizes(q, k, v, lengths):
     return views, (B, heads, kv, N, M, d), _dtype_code(q)
 
 
-def _cross_work(q, sizes, code, backward):
-    """A workspace for one call (None where it needs none) and its bytes."""
+@lru_cache(maxsize=1024)
+def _work_bytes(device: int, fn: str, *sizes) -> int:
+    """What a workspace query answers for these sizes on a device (a call of it takes as
+    long as a third of a launch)."""
     n = ctypes.c_int64()
-    _on_device_of(q, lib().hla_cross_attn_workspace, *sizes, code, backward, ctypes.byref(n))
-    return (q.new_empty(n.value, dtype=torch.uint8) if n.value else None), n.value
+    with torch.cuda.device(device):
+        _check(getattr(lib(), fn)(*sizes, ctypes.byref(n)))
+    return n.value
+
+
+def _work(t: torch.Tensor, fn: str, *sizes):
+    """A workspace for one call on t's device (None where it needs none) and its bytes."""
+    n = _work_bytes(t.get_device(), fn, *sizes)
+    return (torch.empty(n, dtype=torch.uint8, device=t.device) if n else None), n
 
 
 def _lse_of(lse, q):
@@ -845,8 +855,8 @@ def cross_attn_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     if lse is not None:
         _lse_of(lse, q)
     elif with_lse:
-        lse = q.new_empty(q.shape[:3], dtype=torch.float32)
-    work, n = _cross_work(q, sizes, code, 0)
+        lse = torch.empty(sizes[0], sizes[1], sizes[3], dtype=torch.float32, device=q.device)
+    work, n = _work(q, "hla_cross_attn_workspace", *sizes, code, 0)
     _call(q, lib().hla_cross_attn_fwd, qv, kv, vv, _ptr(lengths), ov, _ptr(lse), *sizes, code,
           1.0 / float(q.shape[3]) ** 0.5 if scale is None else float(scale), _ptr(work), n)
     return out, lse
@@ -868,7 +878,7 @@ def cross_attn_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch
     dq, dqv = _rows_like(dq, "dq", q)
     dk, dkv = _rows_like(dk, "dk", k)
     dv, dvv = _rows_like(dv, "dv", v)
-    work, n = _cross_work(q, sizes, code, 1)
+    work, n = _work(q, "hla_cross_attn_workspace", *sizes, code, 1)
     _call(q, lib().hla_cross_attn_bwd, qv, kv, vv, _rows(out, "out", q), _rows(dout, "dout", q), _ptr(lse),
           _ptr(lengths), dqv, dkv, dvv, *sizes, code,
           1.0 / float(q.shape[3]) ** 0.5 if scale is None else float(scale), _ptr(work), n)
@@ -903,13 +913,6 @@ def _shaped(t, name, like, shape):
     return t
 
 
-def _linear_work(x, T, K, F, act_code, code, backward):
-    """A workspace for one call (None where it needs none) and its bytes."""
-    n = ctypes.c_int64()
-    _on_device_of(x, lib().hla_linear_workspace, T, K, F, act_code, code, backward, ctypes.byref(n))
-    return (x.new_empty(n.value, dtype=torch.uint8) if n.value else None), n.value
-
-
 def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
            residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
            pre: Optional[torch.Tensor] = None, with_pre: bool = False):
@@ -928,7 +931,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     if with_pre or pre is not None:
         pre = _shaped(pre, "pre", x, shape)
     # (up to 64 tokens it needs none)
-    work, n = _linear_work(x, T, K, F, act_code, code, 0) if T > 64 else (None, 0)
+    work, n = _work(x, "hla_linear_workspace", T, K, F, act_code, code, 0) if T > 64 else (None, 0)
     _call(x, lib().hla_linear, _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), act_code, _ptr(out),
           _ptr(pre), T, K, F, code, _ptr(work), n)
     return out if pre is None else (out, pre)
@@ -952,7 +955,7 @@ def linear_bwd(x: torch.Tensor, w: torch.Tensor, dy: torch.Tensor, pre: Optional
     dw = _shaped(dw, "dw", x, w.shape)
     if with_bias or db is not None:
         db = _shaped(db, "db", x, (F,))
-    work, n = _linear_work(x, T, K, F, act_code, code, 1)
+    work, n = _work(x, "hla_linear_workspace", T, K, F, act_code, code, 1)
     _call(x, lib().hla_linear_bwd, _ptr(x), _ptr(w), _ptr(pre) if act_code else 0, _ptr(dy), act_code,
           _ptr(dx), _ptr(dw), _ptr(db), T, K, F, code, _ptr(work), n)
     return dx, dw, db
