@@ -524,22 +524,41 @@ struct BwdRows {
     Tl::load(out, row_ptr<T>(a.out, a.os, b, rw), half);
     lraw = a.lse[(int64_t)bk * a.R + rc];
   }
-  // The statistics, kept and stored for the dk / dv kernel: lse log2 e (+inf for a row
-  // without a key and for the padding of the last tile, which makes every weight
-  // exp2(s - inf) = 0) and -delta.
-  __device__ __forceinline__ void finish(const CrossArgs &a, int bk, int r, int half, bool keep = true) {
+  // The statistics: lse log2 e (+inf for a row without a key and for the padding of the
+  // last tile, which makes every weight exp2(s - inf) = 0) and -delta.
+  __device__ __forceinline__ void finish(const CrossArgs &a, int r) {
     const float d = Tl::dot(out, g);
     ndelta = -(d + __shfl_xor(d, 32));
     lse2 = r < a.R && lraw != -__builtin_inff() ? lraw * kLog2e : __builtin_inff();
-    if (half == 0 && keep) {
-      const int64_t at = (int64_t)bk * a.Rp + r;
-      a.stats[at] = lse2;
-      a.stats[(int64_t)a.B * a.kv * a.Rp + at] = ndelta;
-    }
   }
-  // acc += dS K over the `left` keys of a tile (K tile, then V tile, at st)
-  __device__ __forceinline__ void tile(const Tl &tl, const char *st, float scale, int left, int half,
-                                       f32x16 (&acc)[Tl::NDB]) const {
+  // ... stored for the dk / dv kernel.
+  __device__ __forceinline__ void keep(const CrossArgs &a, int bk, int r, int half) const {
+    if (half) return;
+    const int64_t at = (int64_t)bk * a.Rp + r;
+    a.stats[at] = lse2;
+    a.stats[(int64_t)a.B * a.kv * a.Rp + at] = ndelta;
+  }
+  // bf16: <dout, out> takes the rounding of out into delta, for all keys alike, and
+  // where few keys share a row's weight, dS = P (dP - delta) cancels and is left with
+  // it (dq and dk of 3 and 20 keys 3.1e-3 off in the 2-norm instead of 2.3e-3, of one to
+  // three keys 4.4e-3). As the weights sum to 1, the sum of a row's dS is just what its
+  // delta lacks. Where a row may see few keys the sum `excess` is taken along, and
+  //   dq = scale (sum_j dS_j k_j - excess sum_j P_j k_j),
+  // the second product beside the first; delta is put right for dk.
+  static constexpr bool kMends = sizeof(T) == 2;
+  struct Sums {
+    f32x16 ds[Tl::NDB], p[Tl::NDB];
+    float excess;
+    __device__ __forceinline__ void init() {
+#pragma unroll
+      for (int db = 0; db < Tl::NDB; ++db) ds[db] = p[db] = f32x16{};
+      excess = 0.f;
+    }
+  };
+  // Sums over the `left` keys of a tile (K tile, then V tile, at st).
+  // MEND: with the excess and the second product. DRY: the excess alone.
+  template <bool MEND, bool DRY = false>
+  __device__ __forceinline__ void tile(const Tl &tl, const char *st, float scale, int left, int half, Sums &sum) const {
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       if (32 * kb >= left) break;
@@ -549,16 +568,37 @@ struct BwdRows {
       tl.rows_times(blk + BN * Tl::ROW, g, dp);
       if (left < 32 * kb + 32) mask_tail(s, left - 32 * kb, half);
 #pragma unroll
-      for (int v = 0; v < 16; ++v)
-        s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], scale, -lse2)) * (dp[v] + ndelta);
-      tl.cols_times(blk, s, acc);
+      for (int v = 0; v < 16; ++v) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], scale, -lse2));
+        s[v] = p * (dp[v] + ndelta);
+        if (MEND || DRY) sum.excess += s[v];
+        dp[v] = p;
+      }
+      if (!DRY) tl.cols_times(blk, s, sum.ds);
+      if (MEND) tl.cols_times(blk, dp, sum.p);
+    }
+  }
+  // The row's whole excess (half: this lane's part of it) into delta and the sums.
+  template <bool MEND>
+  __device__ __forceinline__ void mend(Sums &sum) {
+    const float excess = sum.excess + __shfl_xor(sum.excess, 32);
+    ndelta -= excess;
+    if (MEND) {
+#pragma unroll
+      for (int db = 0; db < Tl::NDB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sum.ds[db][v] = __builtin_fmaf(-excess, sum.p[db][v], sum.ds[db][v]);
     }
   }
 };
 
+// Keys up to which cross_dq mends delta, in a pass of its own (it has no registers for
+// the second product). Beyond, the rounding of out is below 3% of the result's error.
+constexpr int kMendKeys = 256;
+
 // dq, and the rows' statistics for the next kernel. Many rows: as cross_fwd.
 template <typename T, int D>
-__global__ void __launch_bounds__(256, 2) cross_dq(CrossArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) cross_dq(CrossArgs a) {
   using Tl = Tile<T, D>;
   constexpr int NDB = Tl::NDB, RING = fwd_ring<T, D>(), NW = 4;
   constexpr int STAGE = 2 * BN * Tl::ROW;
@@ -578,33 +618,44 @@ __global__ void __launch_bounds__(256, 2) cross_dq(CrossArgs a) {
     const int at = i * BN;
     Copy::issue(K + (int64_t)at * kr, V + (int64_t)at * vr, kr, vr, len - 1 - at, lds + (i % RING) * STAGE, wave, lane);
   };
-#pragma unroll
-  for (int i = 0; i < RING - 1; ++i)
-    if (i < nt) issue(i);
   const int r0 = (rt * NW + wave) * 32;
   BwdRows<T, D> rows;
-  rows.load(a, bk, b, kvh, r0 + col, half);
-  wait_vmem_all();
-  rows.finish(a, bk, r0 + col, half);
   Tl tl;
   tl.init(lane);
-  f32x16 acc[NDB];
+  typename BwdRows<T, D>::Sums sum;
+  sum.init();
+  auto start = [&]() {
 #pragma unroll
-  for (int db = 0; db < NDB; ++db) acc[db] = f32x16{};
-  for (int i = 0; i < nt; ++i) {
-    wait_tiles_then_barrier<Copy::LPT, RING - 2>(min(RING - 2, nt - 1 - i));
-    if (i + RING - 1 < nt) issue(i + RING - 1);
-    rows.tile(tl, lds + (i % RING) * STAGE, a.scale_log2, len - i * BN, half, acc);
+    for (int i = 0; i < RING - 1; ++i)
+      if (i < nt) issue(i);
+  };
+  auto walk = [&](auto f) __attribute__((always_inline)) {
+    for (int i = 0; i < nt; ++i) {
+      wait_tiles_then_barrier<Copy::LPT, RING - 2>(min(RING - 2, nt - 1 - i));
+      if (i + RING - 1 < nt) issue(i + RING - 1);
+      f(lds + (i % RING) * STAGE, len - i * BN);
+    }
+    wait_then_barrier<0>();   // every wave is done with the ring
+  };
+  start();
+  rows.load(a, bk, b, kvh, r0 + col, half);
+  wait_vmem_all();
+  rows.finish(a, r0 + col);
+  if (rows.kMends && len <= kMendKeys) {
+    walk([&](const char *st, int left) { rows.template tile<false, true>(tl, st, a.scale_log2, left, half, sum); });
+    rows.template mend<false>(sum);
+    start();
   }
-  wait_then_barrier<0>();
-  store_rows<T, D>(lds + wave * AREA, acc, a.scale, lane, [&](int i) {
+  walk([&](const char *st, int left) { rows.template tile<false>(tl, st, a.scale_log2, left, half, sum); });
+  rows.keep(a, bk, r0 + col, half);
+  store_rows<T, D>(lds + wave * AREA, sum.ds, a.scale, lane, [&](int i) {
     return r0 + i < a.R ? row_ptr<T>(a.dq, a.dqs, b, row_of(a, r0 + i, kvh)) : nullptr;
   });
 }
 
 // Few rows: as cross_fwd_few.
 template <typename T, int D>
-__global__ void __launch_bounds__(256, 1) cross_dq_few(CrossArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) * D <= 64 ? 2 : 1) cross_dq_few(CrossArgs a) {
   using Tl = Tile<T, D>;
   using Few = FewRows<T, D>;
   constexpr int NDB = Tl::NDB;
@@ -620,30 +671,44 @@ __global__ void __launch_bounds__(256, 1) cross_dq_few(CrossArgs a) {
   const int r0 = rt * 32;
   BwdRows<T, D> rows;
   rows.load(a, bk, b, kvh, r0 + col, half);
-  rows.finish(a, bk, r0 + col, half, wave == 0);
+  rows.finish(a, r0 + col);
   Tl tl;
   tl.init(lane);
-  f32x16 acc[NDB];
-#pragma unroll
-  for (int db = 0; db < NDB; ++db) acc[db] = f32x16{};
-  few.walk(wave, lane, [&](const char *st, int left) { rows.tile(tl, st, a.scale_log2, left, half, acc); });
+  constexpr bool MEND = BwdRows<T, D>::kMends;
+  constexpr int PER = ((MEND ? 2 : 1) * 16 * NDB + 1) * 64;   // floats that a wave hands over
+  static_assert(3 * PER * 4 + 32 * (Tl::ROW + 16) <= Few::LDSB, "the waves' sums and the rows' staging must fit the rings");
+  typename BwdRows<T, D>::Sums sum;
+  sum.init();
+  few.walk(wave, lane, [&](const char *st, int left) { rows.template tile<MEND>(tl, st, a.scale_log2, left, half, sum); });
   wait_then_barrier<0>();
   float *ex = reinterpret_cast<float *>(lds) + lane;
-  auto at = [&](int w, int i) { return (w - 1) * (Few::PER / 4) + i * 64; };
-#pragma unroll
-  for (int db = 0; db < NDB; ++db)
-#pragma unroll
-    for (int v = 0; v < 16; ++v)
-      if (wave) ex[at(wave, 16 * db + v)] = acc[db][v];
-  wait_then_barrier<0>();
-  if (wave) return;
-#pragma unroll
-  for (int w = 1; w < 4; ++w)
+  auto at = [&](int w, int i) { return (w - 1) * PER + i * 64; };
+  if (wave) {
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) acc[db][v] += ex[at(w, 16 * db + v)];
-  store_rows<T, D>(lds + 3 * Few::PER, acc, a.scale, lane, [&](int i) {
+      for (int v = 0; v < 16; ++v) {
+        ex[at(wave, 16 * db + v)] = sum.ds[db][v];
+        if (MEND) ex[at(wave, 16 * (NDB + db) + v)] = sum.p[db][v];
+      }
+    ex[at(wave, PER / 64 - 1)] = sum.excess;
+  }
+  wait_then_barrier<0>();
+  if (wave) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) {
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        sum.ds[db][v] += ex[at(w, 16 * db + v)];
+        if (MEND) sum.p[db][v] += ex[at(w, 16 * (NDB + db) + v)];
+      }
+    sum.excess += ex[at(w, PER / 64 - 1)];
+  }
+  if (MEND) rows.template mend<true>(sum);
+  rows.keep(a, bk, r0 + col, half);
+  store_rows<T, D>(lds + 3 * PER * 4, sum.ds, a.scale, lane, [&](int i) {
     return r0 + i < a.R ? row_ptr<T>(a.dq, a.dqs, b, row_of(a, r0 + i, kvh)) : nullptr;
   });
 }
@@ -676,14 +741,16 @@ __global__ void __launch_bounds__(256, short_waves(sizeof(T) * D)) cross_dq_shor
   wait_then_barrier<0>();
   for (; rb < nblk; rb += step) {
     const int r0 = rb * 32;
-    rows.finish(a, bk, r0 + col, half);
+    rows.finish(a, r0 + col);
     BwdRows<T, D> next;
     next.load(a, bk, b, kvh, min(rb + step, nblk - 1) * 32 + col, half);
-    f32x16 acc[NDB];
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) acc[db] = f32x16{};
-    for (int i = 0; i < nt; ++i) rows.tile(tl, lds + i * STAGE, a.scale_log2, len - i * BN, half, acc);
-    store_rows<T, D>(lds + 2 * STAGE + wave * AREA, acc, a.scale, lane, [&](int i) {
+    constexpr bool MEND = BwdRows<T, D>::kMends;
+    typename BwdRows<T, D>::Sums sum;
+    sum.init();
+    for (int i = 0; i < nt; ++i) rows.template tile<MEND>(tl, lds + i * STAGE, a.scale_log2, len - i * BN, half, sum);
+    if (MEND) rows.template mend<true>(sum);
+    rows.keep(a, bk, r0 + col, half);
+    store_rows<T, D>(lds + 2 * STAGE + wave * AREA, sum.ds, a.scale, lane, [&](int i) {
       return r0 + i < a.R ? row_ptr<T>(a.dq, a.dqs, b, row_of(a, r0 + i, kvh)) : nullptr;
     });
     rows = next;
