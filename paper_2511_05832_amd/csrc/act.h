@@ -20,14 +20,24 @@ __device__ __forceinline__ float normal_tail(float z, float &density) {
   return 0.5f * p * t * e;
 }
 
-// gelu(z) = max(z, 0) - |z| Phi(-|z|) with the same formula. |z| is taken up to 88, where
-// the tail is 0 already: inf * 0 must not be formed. (v_med3 takes one instruction where
-// fminf takes two; a NaN comes back through the exponential.)
+// gelu(z) = max(z, 0) - |z| Phi(-|z|), with log2 Phi(-a) a polynomial: smooth, from -1 at 0
+// to the parabola of the tail, so one exponential and no reciprocal. The coefficients are
+// the minimax fit on 0 <= a <= 8 of the larger of the tail's error over 3e-7 and its
+// relative error over 1e-4 (a linear programme on 2400 points); Phi is within 3.1e-7, and
+// gelu within 1e-4 of itself down to 1e-8, against bf16's half step of 2^-8. Past 8 the
+// polynomial stays below -50 and falls. 12 instructions, 7.1.26 takes 17 here, and a
+// layer's epilogue is bound by their issue.
+// |z| is taken up to 64: inf * 0 must not be formed. (minimum and maximum hand NaN on.)
 __device__ __forceinline__ float gelu_fast(float z) {
-  const float a = __builtin_amdgcn_fmed3f(fabsf(z), 0.f, 88.f);
-  float density;
-  const float tail = normal_tail(z, density);
-  return __builtin_fmaf(-a, tail, __builtin_amdgcn_fmed3f(z, 0.f, __builtin_inff()));
+  const float a = __builtin_elementwise_minimum(__builtin_fabsf(z), 64.f);
+  float q = __builtin_fmaf(-7.49217696e-7f, a, 4.20198360e-5f);
+  q = __builtin_fmaf(q, a, -7.97152815e-4f);
+  q = __builtin_fmaf(q, a, 8.08079023e-3f);
+  q = __builtin_fmaf(q, a, -5.33045511e-2f);
+  q = __builtin_fmaf(q, a, -4.58911025e-1f);
+  q = __builtin_fmaf(q, a, -1.15114427f);
+  q = __builtin_fmaf(q, a, -0.999999204f);
+  return __builtin_fmaf(-a, __builtin_amdgcn_exp2f(q), __builtin_elementwise_maximum(z, 0.f));
 }
 
 // EXACT: fp32 results.

@@ -131,7 +131,7 @@ struct Reader {
   }
 };
 
-constexpr int kGroup = 4;   // tiles along NA that are walked together
+constexpr int kGroup = 8;   // tiles along NA that are walked together (4: 2% slower, 16384 x 4096 by 1024)
 
 enum Epilogue { EPI_LAYER = 0, EPI_PLAIN = 1, EPI_PART = 2 };
 
@@ -140,40 +140,44 @@ struct GemmArgs {
   int64_t lda, ldb;          // elements between memory rows
   int32_t NA, NB, KC;        // output columns, rows; contraction
   int32_t stages;            // stages per split
-  const void *bias, *residual;
-  void *out, *pre;
+  const void *bias;
+  void *residual, *out, *pre;
   float *part;               // [splits, NB, NA]
   int32_t act;
   int32_t na;                // tiles along NA
   FastDiv gdiv, tdiv;        // division by the tiles of a group, and by all tiles of a split
 };
 
-// V consecutive results of the layer from z before its bias (fp32) on.
 template <typename T>
 using Vec = T __attribute__((ext_vector_type(Type<T>::V)));
 // A result's chunk past the caches (16384 x 4096 results with their z and a residual 194
 // -> 182 us).
 template <typename T>
-__device__ __forceinline__ void store_through(T *p, const Vec<T> &v) {
+__device__ __forceinline__ void store_through(T *p, const T &v) {
   __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4 *>(p));
 }
 template <typename T>
-__device__ __forceinline__ Vec<T> bias_of(const GemmArgs &p, int f) {
-  return p.bias ? *reinterpret_cast<const Vec<T> *>(static_cast<const T *>(p.bias) + f) : Vec<T>{};
-}
-template <typename T>
-__device__ __forceinline__ void finish(const GemmArgs &p, float (&z)[Type<T>::V], const Vec<T> &bias,
-                                       const Vec<T> &residual, int64_t row, int f) {
-  constexpr int V = Type<T>::V;
-  typedef Vec<T> vec;
-  const int64_t at = row * p.NA + f;
+__device__ __forceinline__ void add_bias(const GemmArgs &p, int f, float (&z)[Type<T>::V]) {
+  if (!p.bias) return;
+  const Vec<T> b = *reinterpret_cast<const Vec<T> *>(static_cast<const T *>(p.bias) + f);
 #pragma unroll
-  for (int e = 0; e < V; ++e) z[e] += (float)bias[e];
-  vec o;
+  for (int e = 0; e < Type<T>::V; ++e) z[e] += (float)b[e];
+}
+// The chunk at byte `off` from row `row` (the same for a wave, and its address scalar) on.
+template <typename T>
+__device__ __forceinline__ Vec<T> *chunk(const GemmArgs &p, void *out, int row, uint32_t off) {
+  return reinterpret_cast<Vec<T> *>(static_cast<char *>(out) + (int64_t)row * p.NA * (int)sizeof(T) + off);
+}
+// V consecutive results of the layer from z (fp32) on.
+template <typename T>
+__device__ __forceinline__ void finish(const GemmArgs &p, float (&z)[Type<T>::V], const Vec<T> &residual, int row,
+                                       uint32_t off) {
+  constexpr int V = Type<T>::V;
+  Vec<T> o;
   if (p.pre) {
 #pragma unroll
     for (int e = 0; e < V; ++e) o[e] = (T)z[e];
-    store_through(static_cast<T *>(p.pre) + at, o);
+    store_through(chunk<T>(p, p.pre, row, off), o);
   }
   apply_act<sizeof(T) == 4>(p.act, z);
   if (p.residual) {
@@ -182,13 +186,13 @@ __device__ __forceinline__ void finish(const GemmArgs &p, float (&z)[Type<T>::V]
   }
 #pragma unroll
   for (int e = 0; e < V; ++e) o[e] = (T)z[e];
-  store_through(static_cast<T *>(p.out) + at, o);
+  store_through(chunk<T>(p, p.out, row, off), o);
 }
 
 // Output tiles of TB rows by TA columns by WA x WB waves, a ring of RING stages of KB
 // bytes of every row.
 template <typename T, int TA, int TB, int WA, int WB, int KB, int RING, bool AT, bool BT, int EPI>
-__global__ void __launch_bounds__(64 * WA * WB, 2) gemm_kernel(GemmArgs p) {
+__global__ void __launch_bounds__(64 * WA * WB, (KB == 64 ? 8 : 2)) gemm_kernel(GemmArgs p) {
   constexpr int NT = 64 * WA * WB, V = Type<T>::V, KT = KB / (int)sizeof(T);
   constexpr int AB = TA / WA / 32, BB = TB / WB / 32;
   using OA = Operand<T, TA, AT, NT, KB>;
@@ -197,8 +201,8 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) gemm_kernel(GemmArgs p) {
   static_assert(LPT * (RING - 2) < 64, "vmcnt range");
   constexpr int STAGE = OA::BYTES + OB::BYTES;
   constexpr int PITCH = TA + 4;                       // floats of a staged output row
-  static_assert(WB * 32 * PITCH * 4 <= RING * STAGE, "the staged rows must fit the ring");
-  __shared__ __attribute__((aligned(16))) char lds[RING * STAGE];
+  constexpr int LDS = RING * STAGE > WB * 32 * PITCH * 4 ? RING * STAGE : WB * 32 * PITCH * 4;
+  __shared__ __attribute__((aligned(16))) char lds[LDS];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
@@ -227,15 +231,28 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) gemm_kernel(GemmArgs p) {
   Reader<T, TB, BT, BB, KB> rb;
   ra.init(wa * 32 * AB, lane);
   rb.init(wb * 32 * BB, lane);
+  // The sums start at the bias: slots 4 g .. + 3 of block x are columns 8 g + 4 half .. of it.
+  f32x16 start[AB] = {};
+  if constexpr (EPI == EPI_LAYER) {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    if (p.bias) {
+#pragma unroll
+      for (int i = 0; i < 4 * AB; ++i) {
+        const int f = a0 + (wa * AB + i / 4) * 32 + 8 * (i % 4) + 4 * half;
+        const T4 v = f < p.NA ? *reinterpret_cast<const T4 *>(static_cast<const T *>(p.bias) + f) : T4{};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) start[i / 4][i % 4 * 4 + e] = (float)v[e];
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < RING - 1; ++i)
+    if (i < ns) issue(i);
   f32x16 acc[AB][BB];
 #pragma unroll
   for (int x = 0; x < AB; ++x)
 #pragma unroll
-    for (int y = 0; y < BB; ++y) acc[x][y] = f32x16{};
-
-#pragma unroll
-  for (int i = 0; i < RING - 1; ++i)
-    if (i < ns) issue(i);
+    for (int y = 0; y < BB; ++y) acc[x][y] = start[x];
   for (int i = 0; i < ns; ++i) {
     // stage i has landed, and every wave is done with stage i - 1
     wait_tiles_then_barrier<LPT, RING - 2>(min(RING - 2, ns - 1 - i));
@@ -263,23 +280,23 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) gemm_kernel(GemmArgs p) {
   float *stage = reinterpret_cast<float *>(lds);
   constexpr int W = EPI == EPI_PART ? 4 : V;       // values per lane and store
   constexpr int CPR = TA / W, ROWS = WB * 32, IT = ROWS * CPR / NT;
-  static_assert(ROWS * CPR % NT == 0 && NT % CPR == 0, "stores must split evenly, a lane's all in one column chunk");
-  const int c = (int)threadIdx.x % CPR, f = a0 + c * W;
-  // (row of this lane's store j of pass y)
+  static_assert(ROWS * CPR % NT == 0 && NT % CPR == 0 && 32 % (NT / CPR) == 0,
+                "stores must split evenly, a lane's all in one column chunk and one row of a run");
+  const int c = (int)threadIdx.x % CPR, f = a0 + c * W, lr = (int)threadIdx.x / CPR;
+  // Store j of pass y: row row_at(y, j) + lr, whose first part is the same for all lanes.
   auto row_at = [&](int y, int j) {
-    const int r = (j * NT + (int)threadIdx.x) / CPR;
+    const int r = j * (NT / CPR);
     return b0 + (r >> 5) * 32 * BB + 32 * y + (r & 31);
   };
-  Vec<T> bias = {}, res[IT] = {};
-  if (EPI == EPI_LAYER && f < p.NA) bias = bias_of<T>(p, f);
+  const uint32_t off = (uint32_t)(lr * p.NA + f) * (uint32_t)(EPI == EPI_PART ? 4 : sizeof(T));
+  Vec<T> res[IT] = {};
 #pragma unroll
   for (int y = 0; y < BB; ++y) {
     if constexpr (EPI == EPI_LAYER) {   // the residual's rows, in flight while the pass is staged
       if (p.residual) {
 #pragma unroll
         for (int j = 0; j < IT; ++j)
-          if (row_at(y, j) < p.NB && f < p.NA)
-            res[j] = *reinterpret_cast<const Vec<T> *>(static_cast<const T *>(p.residual) + (int64_t)row_at(y, j) * p.NA + f);
+          if (lr < p.NB - row_at(y, j) && f < p.NA) res[j] = *chunk<T>(p, p.residual, row_at(y, j), off);
       }
     }
     wait_then_barrier<63>();
@@ -293,21 +310,22 @@ __global__ void __launch_bounds__(64 * WA * WB, 2) gemm_kernel(GemmArgs p) {
 #pragma unroll
     for (int j = 0; j < IT; ++j) {
       const int row = row_at(y, j);
-      if (row >= p.NB || f >= p.NA) continue;
-      const float *src = stage + (j * NT + (int)threadIdx.x) / CPR * PITCH + c * W;
+      if (lr >= p.NB - row || f >= p.NA) continue;
+      const float *src = stage + (j * (NT / CPR) + lr) * PITCH + c * W;
       if constexpr (EPI == EPI_PART) {
-        *reinterpret_cast<f32x4 *>(p.part + ((int64_t)sp * p.NB + row) * p.NA + f) = *reinterpret_cast<const f32x4 *>(src);
+        char *dst = reinterpret_cast<char *>(p.part + ((int64_t)sp * p.NB + row) * p.NA);
+        *reinterpret_cast<f32x4 *>(dst + off) = *reinterpret_cast<const f32x4 *>(src);
       } else {
         float z[V];
 #pragma unroll
         for (int e = 0; e < V; e += 4) *reinterpret_cast<f32x4 *>(z + e) = *reinterpret_cast<const f32x4 *>(src + e);
         if constexpr (EPI == EPI_LAYER) {
-          finish<T>(p, z, bias, res[j], row, f);
+          finish<T>(p, z, res[j], row, off);
         } else {
           Vec<T> o;
 #pragma unroll
           for (int e = 0; e < V; ++e) o[e] = (T)z[e];
-          store_through(static_cast<T *>(p.out) + (int64_t)row * p.NA + f, o);
+          store_through(chunk<T>(p, p.out, row, off), o);
         }
       }
     }
@@ -402,8 +420,10 @@ __global__ void __launch_bounds__(64 * kFewWaves) few_kernel(GemmArgs p) {
       for (int j = 0; j < 4; ++j) z[e + j] = s[j];
     }
     Vec<T> r = {};
-    if (p.residual) r = *reinterpret_cast<const Vec<T> *>(static_cast<const T *>(p.residual) + (int64_t)t * p.NA + f);
-    finish<T>(p, z, bias_of<T>(p, f), r, t, f);
+    const uint32_t off = (uint32_t)f * (uint32_t)sizeof(T);
+    if (p.residual) r = *chunk<T>(p, p.residual, t, off);
+    add_bias<T>(p, f, z);
+    finish<T>(p, z, r, t, off);
   }
 }
 
@@ -499,8 +519,8 @@ __global__ void __launch_bounds__(256) finish_kernel(GemmArgs p, int n) {
   constexpr int V = Type<T>::V;
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V, len = (int64_t)p.NB * p.NA;
   if (i >= len) return;
-  const int64_t row = i / p.NA;
-  const int f = (int)(i - row * p.NA);
+  const int row = (int)(i / p.NA);
+  const int f = (int)(i - (int64_t)row * p.NA);
   float z[V] = {};
   for (int k = 0; k < n; ++k)
 #pragma unroll
@@ -510,8 +530,10 @@ __global__ void __launch_bounds__(256) finish_kernel(GemmArgs p, int n) {
       for (int j = 0; j < 4; ++j) z[e + j] += x[j];
     }
   Vec<T> r = {};
-  if (p.residual) r = *reinterpret_cast<const Vec<T> *>(static_cast<const T *>(p.residual) + i);
-  finish<T>(p, z, bias_of<T>(p, f), r, row, f);
+  const uint32_t off = (uint32_t)f * (uint32_t)sizeof(T);
+  if (p.residual) r = *chunk<T>(p, p.residual, row, off);
+  add_bias<T>(p, f, z);
+  finish<T>(p, z, r, row, off);
 }
 
 // ---------------------------------------------------------------------------
@@ -519,16 +541,21 @@ __global__ void __launch_bounds__(256) finish_kernel(GemmArgs p, int n) {
 //  fp32: 64 x 64, 128 bytes by 2 stages (32 KiB). The matrix cores are slow enough here
 //    that small tiles keep them busy, and even out (4096 tokens, 1024 -> 1024: 75 us, 128 x
 //    128 79; 192 -> 768: 19 against 30).
-//  bf16: 256 x 256 (128 KiB, one workgroup per CU) where such tiles fill the CUs and the
-//    contraction is long enough to pay for a tile's first stage and its stores: 16384 x
-//    1024 by 4096 contracted 112 us against 131 with 128 x 128; but 65536 x 768 by 192:
-//    54 against 47. Or, where parts are allowed, a quarter of the CUs and over 2048
-//    contracted elements for each part (4096 x 1024 by 16384 in four parts 125 us, 128 x
-//    128 in two 128).
+//  bf16: 256 x 256 (128 KiB, one workgroup per CU) where such tiles fill the CUs. A long
+//    contraction hides a tile's first stage and its epilogue (16384 x 1024 by 4096: 112
+//    us, 128 x 128 131); a short one wants the epilogue beside another workgroup's
+//    products. 65536 tokens, K -> 768, with gelu / without, against 128 x 128 by stages
+//    of 64 bytes: K = 192 48.7 / 35.7 against 44.9 / 39.4 us, K = 256 53.1 / 40.3 against
+//    51.9 / 45.4, K = 384 63.3 / 49.0 against 66.4 / 61.7. So from 256 on, and without an
+//    epilogue from 128 on. Or, where parts are allowed, a quarter of the CUs and over
+//    2048 contracted elements for each part (4096 x 1024 by 16384 in four parts 125 us,
+//    128 x 128 in two 128).
 //    128 x 128 where those are at least three to two CUs, or, in parts, 8 stages for
-//    every workgroup (768 x 192 by 65536: 32 us, 64 x 64 37); two workgroups per CU with
-//    2 stages of 128 bytes, or three with 3 stages of 64 for a layer of a short
-//    contraction (65536 tokens, 192 -> 768: 47 us against 50).
+//    every workgroup (768 x 192 by 65536: 32 us, 64 x 64 37): four waves and 2 stages of
+//    128 bytes, two workgroups per CU; or, for a layer of a short contraction with tiles
+//    for four, eight waves and 2 stages of 64 bytes, four workgroups per CU (65536 tokens,
+//    192 -> 768, gelu: 44.9 us against 49.7; at two to a CU, 8192 tokens, 192 -> 1024:
+//    12.1 against 11.6).
 //    64 x 64 by 4 stages otherwise (2048 tokens, 1024 -> 1024: 11 us, 128 x 128 16).
 // Parts: as many as fill the CUs' workgroups, of at least four stages each.
 struct Plan {
@@ -551,9 +578,10 @@ Plan plan_of(int64_t NA, int64_t NB, int64_t KC, bool layer, bool parts) {
   if (sizeof(T) == 4) return make(64, 128, 2 * cus, 4);
   const int64_t n256 = tiles(256), n128 = tiles(128);
   const bool fills = n256 * 5 >= (n256 + cus - 1) / cus * cus * 4;   // four fifths of its rounds
-  if (KC >= 512 && fills) return make(256, 128, cus, 4);
+  if (KC >= (layer ? 256 : 128) && fills) return make(256, 128, cus, 4);
   if (parts && !layer && 4 * n256 >= cus && KC * n256 / cus >= 2048) return make(256, 128, cus, 4);
-  if (2 * n128 >= 3 * cus) return layer && KC < 512 ? make(128, 64, 1, 1) : make(128, 128, 2 * cus, 4);
+  if (layer && KC < 256 && n128 >= 4 * cus) return make(128, 64, 1, 1);
+  if (2 * n128 >= 3 * cus) return make(128, 128, 2 * cus, 4);
   if (parts && !layer && n128 * ((KC + 63) / 64) >= 16 * cus) return make(128, 128, 2 * cus, 4);
   return make(64, 128, 2 * cus, layer ? 8 : 4);
 }
@@ -576,7 +604,7 @@ hipError_t launch_gemm(GemmArgs &p, const Plan &plan, hipStream_t s) {
     } else if (plan.kb == 128) {
       hipLaunchKernelGGL((gemm_kernel<T, 128, 128, 2, 2, 128, 2, AT, BT, EPI>), grid, dim3(256), 0, s, p);
     } else if constexpr (EPI == EPI_LAYER) {
-      hipLaunchKernelGGL((gemm_kernel<T, 128, 128, 2, 2, 64, 3, AT, BT, EPI>), grid, dim3(256), 0, s, p);
+      hipLaunchKernelGGL((gemm_kernel<T, 128, 128, 4, 2, 64, 2, AT, BT, EPI>), grid, dim3(512), 0, s, p);
     }
   }
   return hipGetLastError();
@@ -605,7 +633,7 @@ hipError_t fwd(const LinearArgs &a, hipStream_t s) {
   p.NB = a.T;
   p.KC = a.K;
   p.bias = a.bias;
-  p.residual = a.residual;
+  p.residual = const_cast<void *>(a.residual);
   p.out = a.y;
   p.pre = a.pre;
   p.act = a.act;

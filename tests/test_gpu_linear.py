@@ -145,6 +145,19 @@ def test_large(size, dtype):
     check_backward(x, w, dy, pre, "gelu", dx, dw, db)
 
 
+# tiles for every CU, the last of each row and column ragged: a short contraction (128 x
+# 128), a longer one (256 x 256), and the same for dx
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [(33000, 72, 520), (7700, 264, 2040), (7700, 2040, 264)], ids=str)
+def test_tiles_for_every_cu(size):
+    x, w, b, r, dy = make(*size, BF, seed=8)
+    y, pre = hla.linear(x, w, b, act="gelu", residual=r, with_pre=True)
+    check_forward(x, w, b, r, "gelu", y, pre)
+    check_forward(x, w, None, None, "silu", hla.linear(x, w, act="silu"), None)
+    dx, dw, db = hla.linear_bwd(x, w, dy, pre, act="gelu", with_bias=True)
+    check_backward(x, w, dy, pre, "gelu", dx, dw, db)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 def test_some_gradients_only(dtype):
