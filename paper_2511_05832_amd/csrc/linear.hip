@@ -191,8 +191,16 @@ __device__ __forceinline__ void finish(const GemmArgs &p, float (&z)[Type<T>::V]
 
 // Output tiles of TB rows by TA columns by WA x WB waves, a ring of RING stages of KB
 // bytes of every row.
+template <typename T, int TA, int TB, int WA, int WB, int KB, int RING>
+struct Shape {
+  static constexpr int PITCH = TA + 4;   // floats of a staged output row
+  static constexpr int RINGS = RING * (TA + TB) * KB, STAGED = WB * 32 * PITCH * 4;
+  static constexpr int LDS = RINGS > STAGED ? RINGS : STAGED;
+};
+
+// Workgroup `block` of `blocks`.
 template <typename T, int TA, int TB, int WA, int WB, int KB, int RING, bool AT, bool BT, int EPI>
-__global__ void __launch_bounds__(64 * WA * WB, (KB == 64 ? 8 : 2)) gemm_kernel(GemmArgs p) {
+__device__ __forceinline__ void gemm_tile(const GemmArgs &p, int block, int blocks, char *lds) {
   constexpr int NT = 64 * WA * WB, V = Type<T>::V, KT = KB / (int)sizeof(T);
   constexpr int AB = TA / WA / 32, BB = TB / WB / 32;
   using OA = Operand<T, TA, AT, NT, KB>;
@@ -200,14 +208,12 @@ __global__ void __launch_bounds__(64 * WA * WB, (KB == 64 ? 8 : 2)) gemm_kernel(
   constexpr int LPT = OA::COPIES + OB::COPIES;
   static_assert(LPT * (RING - 2) < 64, "vmcnt range");
   constexpr int STAGE = OA::BYTES + OB::BYTES;
-  constexpr int PITCH = TA + 4;                       // floats of a staged output row
-  constexpr int LDS = RING * STAGE > WB * 32 * PITCH * 4 ? RING * STAGE : WB * 32 * PITCH * 4;
-  __shared__ __attribute__((aligned(16))) char lds[LDS];
+  constexpr int PITCH = Shape<T, TA, TB, WA, WB, KB, RING>::PITCH;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int wa = wave % WA, wb = wave / WA;
-  const int logical = xcd_remap(blockIdx.x, gridDim.x);
+  const int logical = xcd_remap(block, blocks);
   const int sp = (int)fdiv((uint32_t)logical, p.tdiv), tile = logical - sp * (int)p.tdiv.div;
   // Columns of kGroup tiles, row by row: the workgroups that run at once on an XCD share
   // few slices of either operand, and the group's A tiles stay in its L2.
@@ -329,6 +335,28 @@ __global__ void __launch_bounds__(64 * WA * WB, (KB == 64 ? 8 : 2)) gemm_kernel(
         }
       }
     }
+  }
+}
+
+template <typename T, int TA, int TB, int WA, int WB, int KB, int RING, bool AT, bool BT, int EPI>
+__global__ void __launch_bounds__(64 * WA * WB, (KB == 64 ? 8 : 2)) gemm_kernel(GemmArgs p) {
+  __shared__ __attribute__((aligned(16))) char lds[Shape<T, TA, TB, WA, WB, KB, RING>::LDS];
+  gemm_tile<T, TA, TB, WA, WB, KB, RING, AT, BT, EPI>(p, blockIdx.x, gridDim.x, lds);
+}
+
+// dx and dW of a small layer in one launch (`first` workgroups of dx), in 64 x 64 tiles
+// and possibly parts: neither fills the CUs by itself (part = null: the result itself).
+template <typename T>
+__global__ void __launch_bounds__(256, 2) gemm_pair_kernel(GemmArgs dx, GemmArgs dw, int first) {
+  constexpr int RING = sizeof(T) == 4 ? 2 : 4;
+  __shared__ __attribute__((aligned(16))) char lds[Shape<T, 64, 64, 2, 2, 128, RING>::LDS];
+  const int block = blockIdx.x;
+  if (block < first) {
+    if (dx.part) gemm_tile<T, 64, 64, 2, 2, 128, RING, true, false, EPI_PART>(dx, block, first, lds);
+    else gemm_tile<T, 64, 64, 2, 2, 128, RING, true, false, EPI_PLAIN>(dx, block, first, lds);
+  } else {
+    if (dw.part) gemm_tile<T, 64, 64, 2, 2, 128, RING, true, true, EPI_PART>(dw, block - first, gridDim.x - first, lds);
+    else gemm_tile<T, 64, 64, 2, 2, 128, RING, true, true, EPI_PLAIN>(dw, block - first, gridDim.x - first, lds);
   }
 }
 
@@ -557,7 +585,9 @@ __global__ void __launch_bounds__(256) finish_kernel(GemmArgs p, int n) {
 //    192 -> 768, gelu: 44.9 us against 49.7; at two to a CU, 8192 tokens, 192 -> 1024:
 //    12.1 against 11.6).
 //    64 x 64 by 4 stages otherwise (2048 tokens, 1024 -> 1024: 11 us, 128 x 128 16).
-// Parts: as many as fill the CUs' workgroups, of at least four stages each.
+// Parts: as many as fill the CUs' workgroups, of at least four stages each; fp32 gradients,
+// two of which run at once: three to two CUs (4096 tokens, 192 -> 768, the whole step: 58.1
+// us, with one to a CU 60.0, two 61.0, three 63.8; dx and dW one after the other 65.9).
 struct Plan {
   int tile, kb;   // tile side, bytes of contraction per stage
   int splits;
@@ -575,7 +605,7 @@ Plan plan_of(int64_t NA, int64_t NB, int64_t KC, bool layer, bool parts) {
     p.splits = (int)((stages + p.stages - 1) / p.stages);
     return p;
   };
-  if (sizeof(T) == 4) return make(64, 128, 2 * cus, 4);
+  if (sizeof(T) == 4) return make(64, 128, (layer ? 4 : 3) * cus / 2, 4);
   const int64_t n256 = tiles(256), n128 = tiles(128);
   const bool fills = n256 * 5 >= (n256 + cus - 1) / cus * cus * 4;   // four fifths of its rounds
   if (KC >= (layer ? 256 : 128) && fills) return make(256, 128, cus, 4);
@@ -586,14 +616,19 @@ Plan plan_of(int64_t NA, int64_t NB, int64_t KC, bool layer, bool parts) {
   return make(64, 128, 2 * cus, layer ? 8 : 4);
 }
 
-template <typename T, bool AT, bool BT, int EPI>
-hipError_t launch_gemm(GemmArgs &p, const Plan &plan, hipStream_t s) {
+// Completes the arguments of a product; returns its workgroups.
+uint32_t set_plan(GemmArgs &p, const Plan &plan) {
   const int64_t na = (p.NA + plan.tile - 1) / plan.tile, nb = (p.NB + plan.tile - 1) / plan.tile;
   p.stages = plan.stages;
   p.na = (int32_t)na;
   p.gdiv = make_fastdiv((uint32_t)(kGroup * nb));
   p.tdiv = make_fastdiv((uint32_t)(na * nb));
-  const dim3 grid((uint32_t)(na * nb * plan.splits));
+  return (uint32_t)(na * nb * plan.splits);
+}
+
+template <typename T, bool AT, bool BT, int EPI>
+hipError_t launch_gemm(GemmArgs &p, const Plan &plan, hipStream_t s) {
+  const dim3 grid(set_plan(p, plan));
   if constexpr (sizeof(T) == 4) {
     hipLaunchKernelGGL((gemm_kernel<T, 64, 64, 2, 2, 128, 2, AT, BT, EPI>), grid, dim3(256), 0, s, p);
   } else {
@@ -664,10 +699,10 @@ int dz_rows(const LinearArgs &a, int V) {
 template <typename T>
 hipError_t bwd(const LinearArgs &a, hipStream_t s) {
   constexpr int V = Type<T>::V;
-  const LinearWork w = linear_bwd_work(a, sizeof(T) == 2 ? HLA_BF16 : HLA_F32);
+  const LinearWork at = linear_bwd_work(a, sizeof(T) == 2 ? HLA_BF16 : HLA_F32);
   char *work = static_cast<char *>(a.work);
-  T *dz = reinterpret_cast<T *>(work + w.dz);
-  float *sums = reinterpret_cast<float *>(work + w.sums);
+  T *dz = reinterpret_cast<T *>(work + at.dz);
+  float *sums = reinterpret_cast<float *>(work + at.sums);
   const bool has_act = a.act != HLA_ACT_NONE;
   SumJobs jobs = {};   // dx, dW, db
   hipError_t e;
@@ -680,31 +715,31 @@ hipError_t bwd(const LinearArgs &a, hipStream_t s) {
     if (a.db) jobs.job[2] = sum_job(sums, a.db, a.F, (int)grid.y);
   }
   const void *g = has_act ? static_cast<const void *>(dz) : a.dy;
-  if (a.dx) {
-    GemmArgs p = {};
-    p.a = a.w;
-    p.lda = a.K;
-    p.b = g;
-    p.ldb = a.F;
-    p.NA = a.K;
-    p.NB = a.T;
-    p.KC = a.F;
-    p.out = a.dx;
-    p.part = reinterpret_cast<float *>(work + w.dx);
-    if ((e = product<T, true, false>(p, plan_of<T>(a.K, a.T, a.F, false, true), &jobs.job[0], s)) != hipSuccess) return e;
-  }
-  if (a.dw) {
-    GemmArgs p = {};
-    p.a = a.x;
-    p.lda = a.K;
-    p.b = g;
-    p.ldb = a.F;
-    p.NA = a.K;
-    p.NB = a.F;
-    p.KC = a.T;
-    p.out = a.dw;
-    p.part = reinterpret_cast<float *>(work + w.dw);
-    if ((e = product<T, true, true>(p, plan_of<T>(a.K, a.F, a.T, false, true), &jobs.job[1], s)) != hipSuccess) return e;
+  GemmArgs x = {}, w = {};
+  x.a = a.w;
+  x.lda = w.lda = a.K;
+  x.b = w.b = g;
+  x.ldb = w.ldb = a.F;
+  x.NA = w.NA = a.K;
+  x.NB = w.KC = a.T;
+  x.KC = w.NB = a.F;
+  x.out = a.dx;
+  x.part = reinterpret_cast<float *>(work + at.dx);
+  w.a = a.x;
+  w.out = a.dw;
+  w.part = reinterpret_cast<float *>(work + at.dw);
+  const Plan px = plan_of<T>(x.NA, x.NB, x.KC, false, true), pw = plan_of<T>(w.NA, w.NB, w.KC, false, true);
+  if (a.dx && a.dw && px.tile == 64 && pw.tile == 64) {
+    if (px.splits > 1) jobs.job[0] = sum_job(x.part, x.out, (int64_t)x.NB * x.NA, px.splits);
+    else x.part = nullptr;
+    if (pw.splits > 1) jobs.job[1] = sum_job(w.part, w.out, (int64_t)w.NB * w.NA, pw.splits);
+    else w.part = nullptr;
+    const uint32_t first = set_plan(x, px), second = set_plan(w, pw);
+    hipLaunchKernelGGL((gemm_pair_kernel<T>), dim3(first + second), dim3(256), 0, s, x, w, (int)first);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  } else {
+    if (a.dx && (e = product<T, true, false>(x, px, &jobs.job[0], s)) != hipSuccess) return e;
+    if (a.dw && (e = product<T, true, true>(w, pw, &jobs.job[1], s)) != hipSuccess) return e;
   }
   const int64_t blocks = (int64_t)jobs.job[0].blocks + jobs.job[1].blocks + jobs.job[2].blocks;
   if (!blocks) return hipSuccess;
