@@ -757,6 +757,30 @@ __global__ void __launch_bounds__(256, short_waves(sizeof(T) * D)) cross_dq_shor
   }
 }
 
+// How dk and dv are shared out over a.pieces workgroups (0: one to a key tile): the tiles
+// that hold seen keys, of which only the device knows the number, get as many row splits
+// as make that many workgroups. (Two elements, 4 heads' rows of 4096 against 1000 of 4096
+// keys: 46 us, 138 with the splits of 4096.) a.uneven = 0: there are as many as the rows
+// allow anyway, no lengths, or over 64 elements, and all keys count as seen.
+struct KeyTiles {
+  int all;             // of all batch elements and key heads
+  int before, of;      // before and of batch element `lane`
+};
+__device__ __forceinline__ int tiles_of(const CrossArgs &a, int len) { return (len + (1 << a.kshift) - 1) >> a.kshift; }
+__device__ __forceinline__ KeyTiles key_tiles(const CrossArgs &a, int lane) {
+  const int n = lane < a.B ? tiles_of(a, keys_of(a, lane)) * a.kv : 0;
+  int sum = n;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(sum, o);
+    if (lane >= o) sum += x;
+  }
+  return {__builtin_amdgcn_readlane(sum, 63), sum - n, n};
+}
+__device__ __forceinline__ int splits_of(const CrossArgs &a, int tiles) {
+  return clampi(a.pieces / max(tiles, 1), 1, a.splits);
+}
+
 // dk and dv of KB blocks of 32 keys: wave w takes the keys of block w % KB against part
 // w / KB of the rows of every step (RB blocks of 32; RH parts). Rows come into an LDS
 // ring by the 16-byte DMA; with RH = 2 the parts are added through LDS at the end.
@@ -781,15 +805,31 @@ __global__ void __launch_bounds__(64 * KB * RH, 2) cross_dkdv(CrossArgs a) {
   const int col = lane & 31, half = lane >> 5, kb = wave % KB, rh = wave / KB;
   const int logical = deal(blockIdx.x, a.unit);
   if (logical >= a.total) return;
-  const int kt = logical % a.n_ktiles, t = logical / a.n_ktiles;
-  const int sp = t % a.splits, bk = t / a.splits, b = bk / a.kv, kvh = bk - b * a.kv;
+  // Workgroups go by (batch, key head, split, tile): those side by side share their rows.
+  int splits = 1, per_head = a.n_ktiles, b = 0, in = logical;
+  if (a.uneven) {
+    const KeyTiles kt = key_tiles(a, lane);
+    splits = splits_of(a, kt.all);
+    const uint64_t hit = __ballot(kt.before * splits <= logical && logical < (kt.before + kt.of) * splits);
+    if (!hit) return;
+    b = (int)__builtin_ctzll(hit);
+    in -= __builtin_amdgcn_readlane(kt.before, b) * splits;
+    per_head = __builtin_amdgcn_readlane(kt.of, b) / a.kv;
+  } else {
+    if (a.pieces) splits = splits_of(a, a.B * a.kv * per_head);
+    b = logical / (a.kv * splits * per_head);
+    if (b >= a.B) return;
+    in -= b * a.kv * splits * per_head;
+  }
+  const int t = in / per_head, kt = in - t * per_head, kvh = t / splits, sp = t - kvh * splits, bk = b * a.kv + kvh;
   const int len = keys_of(a, b);
   const int j0 = (kt * KB + kb) * 32, kpos = j0 + col;   // this wave's first key, this lane's
+
   // (no key of the tile is seen: zeros, which the joining launch knows by itself)
-  if (kt * KB * 32 >= len && a.splits > 1) return;
+  if (a.pieces && kt * KB * 32 >= len) return;
 
   // This split's rows: whole steps.
-  const int steps = (a.R + BR - 1) / BR, per = (steps + a.splits - 1) / a.splits;
+  const int steps = (a.R + BR - 1) / BR, per = (steps + splits - 1) / splits;
   const int i0 = min(sp * per, steps), i1 = kt * KB * 32 < len ? min(i0 + per, steps) : i0;
   const float *S = a.stats + (int64_t)bk * a.Rp;
   const int64_t dofs = (int64_t)a.B * a.kv * a.Rp;   // from lse to -delta
@@ -871,9 +911,9 @@ __global__ void __launch_bounds__(64 * KB * RH, 2) cross_dkdv(CrossArgs a) {
     wait_then_barrier<0>();
   }
   auto put = [&](f32x16 (&sum)[NDB], int which) {
-    if (a.splits > 1) {
+    if (a.pieces) {
       if (kpos < len) {
-        float *p = a.part + ((((int64_t)sp * a.B * a.kv + bk) * a.M + kpos) * 2 + which) * D;
+        float *p = a.part + (((int64_t)logical * (32 * KB) + 32 * kb + col) * 2 + which) * D;
         Tl::columns(sum, half, [&](int c, f32x4 x) { *reinterpret_cast<f32x4 *>(p + c) = x; });
       }
       return;
@@ -895,15 +935,25 @@ __global__ void __launch_bounds__(64 * KB * RH, 2) cross_dkdv(CrossArgs a) {
 template <typename T, int D>
 __global__ void __launch_bounds__(256) cross_sum(CrossArgs a) {
   constexpr int TPR = D / 4;
-  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x, keys = (int64_t)a.B * a.kv * a.M;
   const int c = (int)(idx % TPR) * 4, which = (int)(idx / TPR % 2);
-  const int64_t key = idx / (2 * TPR), keys = (int64_t)a.B * a.kv * a.M;
-  if (key >= keys) return;
+  const int64_t key = min(idx / (2 * TPR), keys - 1);   // (every lane takes part in the scan)
   const int bk = (int)(key / a.M), j = (int)(key - (int64_t)bk * a.M), b = bk / a.kv, kvh = bk - b * a.kv;
+  int tiles = a.B * a.kv * a.n_ktiles, per_head = a.n_ktiles, before = b * a.kv * a.n_ktiles;
+  const int len = keys_of(a, b);
+  if (a.uneven) {
+    const KeyTiles kt = key_tiles(a, threadIdx.x & 63);
+    tiles = kt.all;
+    per_head = tiles_of(a, len);
+    before = __shfl(kt.before, b);
+  }
+  if (idx / (2 * TPR) >= keys) return;
   f32x4 sum = {};
-  if (j < keys_of(a, b)) {
-    const float *p = a.part + (key * 2 + which) * D + c;
-    for (int s = 0; s < a.splits; ++s) sum += *reinterpret_cast<const f32x4 *>(p + s * keys * 2 * D);
+  if (j < len) {
+    const int splits = splits_of(a, tiles), piece = (before + kvh * per_head) * splits + (j >> a.kshift);
+    const float *p = a.part + ((((int64_t)piece << a.kshift) + (j & ((1 << a.kshift) - 1))) * 2 + which) * D + c;
+    for (int s = 0; s < splits; ++s)
+      sum += *reinterpret_cast<const f32x4 *>(p + ((int64_t)(s * per_head) << a.kshift) * 2 * D);
   }
   const CrossStride &os = which ? a.dvs : a.dks;
   T *dst = row_ptr<T>(which ? a.dv : a.dk, os, b, {(uint32_t)kvh, (uint32_t)j});
@@ -973,11 +1023,12 @@ hipError_t bwd(CrossArgs &a, hipStream_t s) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 grid = deal_grid(a, bk * a.n_ktiles * a.splits);
-  if (kv_blocks(a) == 2) hipLaunchKernelGGL((cross_dkdv<T, D, 2, 2, RB>), grid, dim3(256), 0, s, a);
+  a.uneven = a.lengths && a.B <= 64 && a.pieces && a.pieces < bk * a.n_ktiles * a.splits;
+  const dim3 grid = deal_grid(a, a.pieces ? a.pieces : bk * a.n_ktiles);
+  if (a.kshift == 6) hipLaunchKernelGGL((cross_dkdv<T, D, 2, 2, RB>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((cross_dkdv<T, D, 4, 2, RB>), grid, dim3(512), 0, s, a);
   e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return e;
+  if (e != hipSuccess || !a.pieces) return e;
   const int64_t n = bk * a.M * 2 * (D / 4);
   hipLaunchKernelGGL((cross_sum<T, D>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, s, a);
   return hipGetLastError();
@@ -1010,15 +1061,18 @@ bool cross_fwd_plan(CrossArgs &a, int row_bytes) {
   return a.splits > 1;
 }
 
-// Row splits of dk and dv: eight waves per CU, at least 128 rows each.
+// dk and dv: eight waves per CU where key tiles alone would leave half of the CUs without
+// work, of at least 128 rows each. (Only the device knows the lengths, and so the splits.)
 bool cross_bwd_plan(CrossArgs &a, int row_bytes) {
-  a.splits = 1;
   a.per = (a.M + BN - 1) / BN * BN;
   share_rows(a, row_bytes);
   const int kb = kv_blocks(a);
+  a.kshift = kb == 2 ? 6 : 7;
   a.n_ktiles = (a.M + 32 * kb - 1) / (32 * kb);
-  a.splits = up_to((int64_t)device_cu_count() * (kb == 2 ? 2 : 1) / ((int64_t)a.B * a.kv * a.n_ktiles), (a.R + 127) / 128);
-  return a.splits > 1;
+  a.splits = (a.R + 127) / 128;
+  const int64_t slots = (int64_t)device_cu_count() * (kb == 2 ? 2 : 1), tiles = (int64_t)a.B * a.kv * a.n_ktiles;
+  a.pieces = a.splits > 1 && 2 * tiles <= slots ? (int)std::min(slots, tiles * a.splits) : 0;
+  return a.pieces > 0;
 }
 
 hipError_t launch_cross_fwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s) {

@@ -208,10 +208,12 @@ struct CrossArgs {
   float *part;                 // partial sums of the splits
   float2 *part_ml;             // forward: their maxima and sums
   int32_t B, heads, kv, G, N, M, R, Rp;
-  // set by the plans: splits of the keys (forward; keys of each) or of the rows (backward),
-  // workgroups that share a list's rows where the keys stay in LDS, dk / dv key tiles
-  int32_t splits, per, row_parts, n_ktiles;
-  int32_t n_rtiles, total, unit;   // set by the launchers: row tiles, pieces of work, run dealt to an XCD
+  // set by the plans: splits of the keys and keys of each (forward) or row splits at most
+  // (backward); workgroups that share a list's rows where the keys stay in LDS; dk / dv:
+  // key tiles of a head, of 2^kshift keys, and workgroups that share the tiles (0: one each)
+  int32_t splits, per, row_parts, n_ktiles, kshift, pieces;
+  // set by the launchers: row tiles, pieces of work, run dealt to an XCD, dk / dv splits by lengths
+  int32_t n_rtiles, total, unit, uneven;
   FastDiv ndiv;                // division by N
   float scale, scale_log2;
 };

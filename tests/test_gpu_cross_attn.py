@@ -133,6 +133,23 @@ def test_forward_and_backward(size, kind, dtype):
         compare(name, g, ref)
 
 
+# the row splits of dk and dv go by what the lengths leave: most of it, little, one key,
+# nothing; and over more batch elements than are looked at
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("size,lengths", [
+    ((5, 2, 1, 2000, 300, 32), [0, 300, 64, 1, 0]), ((5, 2, 1, 2000, 300, 32), [129, 0, 0, 0, 0]),
+    ((5, 2, 1, 2000, 300, 32), [0] * 5), ((3, 2, 2, 4100, 100, 64), [100, 5, 70]),
+    ((70, 1, 1, 1000, 40, 32), [b % 41 for b in range(70)])], ids=str)
+def test_gradients_of_uneven_lengths(size, lengths, dtype):
+    q, k, v, dout = inputs(*size, dtype, seed=9)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    ref = reference(q, k, v, n, size[-1] ** -0.5, dout)
+    out, lse = hla.cross_attn_fwd(q, k, v, n)
+    for name, got in zip(("dq", "dk", "dv"), hla.cross_attn_bwd(q, k, v, out, dout, lse, n)):
+        compare(name, got, ref)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("size", [(2, 4, 2, 40, 77, 64), (4, 6, 6, 1, 200, 32)], ids=str)
