@@ -12,15 +12,23 @@
 // values are read once for the whole group, a token's few heads fill one tile, and the
 // sums over shared heads in dk and dv are sums over rows like any other.
 //
-// Forward: one workgroup per row tile; a wave keeps its 32 queries in registers and
-// walks tiles of 64 keys that come into an LDS ring by the 16-byte LDS DMA, with the
-// running maximum and sum of the softmax. Few rows against many keys: the keys are
-// split over workgroups, whose partial sums (fp32, with their maxima) are joined by a
-// second launch.
-// Backward, two kernels as in the block-sparse backward, no atomics: dq per row tile
-// (it also stores each row's statistics), then dk and dv per tile of 64 keys, the rows
-// split over workgroups where there are few key tiles (fp32 partial sums, added in
-// order by a third launch).
+// Forward, by shape:
+//  many rows    a workgroup per 128 rows; a wave keeps its 32 queries in registers, and the
+//               four walk tiles of 64 keys that come into an LDS ring by the 16-byte LDS
+//               DMA, with the running maximum and sum of the softmax;
+//  few rows     a workgroup per 32 rows, its waves on tiles of their own, and the keys split
+//               over workgroups too, whose partial sums (fp32, with their maxima) a second
+//               launch joins;
+//  few keys     keys and values stay in LDS, and the waves go through blocks of 32 rows.
+// Backward, two kernels as in the block-sparse backward, no atomics: dq in the same three
+// ways (it also stores each row's statistics), then dk and dv per tile of 64 or 128 keys,
+// the rows split over workgroups where there are few key tiles (fp32 partial sums, added
+// in order by a third launch).
+//
+// What bounds them, in heads of 64 with many rows and keys: a wave's exponentials and its
+// matrix products follow one another, at the two or three waves per SIMD that registers and
+// rows allow. 8 heads on 2, 4096 rows and keys, batch 2, bf16: forward 117 us (590 TFLOP/s),
+// dq 130 (790), dk and dv 151 (910).
 //
 // Masked places: keys from length on are never loaded (the last tile's copies stop at
 // the last seen key, of which the others are copies) and get weight 0, so nothing that
@@ -418,7 +426,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) cross_fwd_few(Cro
 
 // Up to 128 keys (a text's tokens): keys and values stay in LDS, and a workgroup's waves,
 // each for itself, go through blocks of 32 rows with the next block's queries in flight.
-// Bound by HBM (q in, out out). (16 x 6 heads of 32, 4096 rows against 77 keys.)
+// Bound by HBM (q in, out out): 16 x 6 heads of 32, 4096 rows against 77 keys 16 us (3.2
+// TB/s; 645 as elementary operations); 4 x 8 heads of 64, 16384 rows 39 us (3.4 TB/s).
 // Workgroups per CU of the kernels whose keys stay in LDS: what their registers (three,
 // two for rows of 128 bytes) or LDS (fp32 rows of 64: 98 KiB, one) leave.
 constexpr int short_waves(int row_bytes) { return row_bytes > 128 ? 1 : (row_bytes > 64 ? 2 : 3); }
@@ -781,13 +790,16 @@ __device__ __forceinline__ int splits_of(const CrossArgs &a, int tiles) {
   return clampi(a.pieces / max(tiles, 1), 1, a.splits);
 }
 
-// dk and dv of KB blocks of 32 keys: wave w takes the keys of block w % KB against part
-// w / KB of the rows of every step (RB blocks of 32; RH parts). Rows come into an LDS
-// ring by the 16-byte DMA; with RH = 2 the parts are added through LDS at the end.
-template <typename T, int D, int KB, int RH, int RB>
-__global__ void __launch_bounds__(64 * KB * RH, 2) cross_dkdv(CrossArgs a) {
+// dk and dv of KB blocks of 32 keys: wave w takes the keys of block w % KB against half
+// w / KB of the rows of every step (RB blocks of 32 each). Rows come into an LDS ring by
+// the 16-byte DMA; the halves are added through LDS at the end. Bound by the waves' vector
+// and matrix work, two waves per SIMD (200 registers): 4096 rows of 8 heads on 2 against
+// 4096 keys, batch 2, heads of 64 in bf16: 151 us (910 TFLOP/s); with 64 keys to a
+// workgroup, and twice the rows' traffic, the whole backward takes 13 us longer.
+template <typename T, int D, int KB, int RB>
+__global__ void __launch_bounds__(128 * KB, 2) cross_dkdv(CrossArgs a) {
   using Tl = Tile<T, D>;
-  constexpr int NDB = Tl::NDB, NW = KB * RH, BR = 32 * RB * RH;   // waves, rows per step
+  constexpr int NDB = Tl::NDB, NW = 2 * KB, BR = 64 * RB;   // waves, rows per step
   constexpr int TILE = BR * Tl::ROW;
   constexpr int STAT = 2 * TILE, STAGE = STAT + BR * 8;
   constexpr int CPW = BR * Tl::CPR / (64 * NW);
@@ -796,7 +808,7 @@ __global__ void __launch_bounds__(64 * KB * RH, 2) cross_dkdv(CrossArgs a) {
   constexpr int LPT = 2 * CPW + 1;
   constexpr int AREA = 32 * (Tl::ROW + 16);
   constexpr int XCH = KB * 2 * NDB * 16 * 64 * 4;
-  constexpr int LDSB = RH == 2 && RING * STAGE < XCH ? XCH : RING * STAGE;
+  constexpr int LDSB = RING * STAGE < XCH ? XCH : RING * STAGE;
   static_assert(NW * AREA <= LDSB && SW <= NW, "staging, statistics");
   static_assert(BR * Tl::CPR % (64 * NW) == 0, "copies must split evenly");
   __shared__ __attribute__((aligned(16))) char lds[LDSB];
@@ -893,42 +905,35 @@ __global__ void __launch_bounds__(64 * KB * RH, 2) cross_dkdv(CrossArgs a) {
     }
   }
 
-  // RH = 2: part 1 hands its dk to part 0 and part 0 its dv to part 1; then each holds
-  // one sum. RH = 1: both are here.
+  // Half 1 hands its dk to half 0, which hands it its dv; then each holds one sum.
   wait_then_barrier<0>();   // every wave is done with the ring
-  if constexpr (RH == 2) {
-    float *xch = reinterpret_cast<float *>(lds);
-    auto at = [&](int which, int db, int e) { return (((kb * 2 + which) * NDB + db) * 16 + e) * 64 + lane; };
+  float *xch = reinterpret_cast<float *>(lds);
+  auto at = [&](int which, int db, int e) { return (((kb * 2 + which) * NDB + db) * 16 + e) * 64 + lane; };
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+  for (int db = 0; db < NDB; ++db)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) xch[at(rh, db, e)] = rh ? dk[db][e] : dv[db][e];
-    wait_then_barrier<0>();
+    for (int e = 0; e < 16; ++e) xch[at(rh, db, e)] = rh ? dk[db][e] : dv[db][e];
+  wait_then_barrier<0>();
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+  for (int db = 0; db < NDB; ++db)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) dk[db][e] = (rh ? dv[db][e] : dk[db][e]) + xch[at(1 - rh, db, e)];
-    wait_then_barrier<0>();
+    for (int e = 0; e < 16; ++e) dk[db][e] = (rh ? dv[db][e] : dk[db][e]) + xch[at(1 - rh, db, e)];
+  wait_then_barrier<0>();
+  if (a.pieces) {
+    if (kpos < len) {
+      float *p = a.part + (((int64_t)logical * (32 * KB) + 32 * kb + col) * 2 + rh) * D;
+      Tl::columns(dk, half, [&](int c, f32x4 x) { *reinterpret_cast<f32x4 *>(p + c) = x; });
+    }
+    return;
   }
-  auto put = [&](f32x16 (&sum)[NDB], int which) {
-    if (a.pieces) {
-      if (kpos < len) {
-        float *p = a.part + (((int64_t)logical * (32 * KB) + 32 * kb + col) * 2 + which) * D;
-        Tl::columns(sum, half, [&](int c, f32x4 x) { *reinterpret_cast<f32x4 *>(p + c) = x; });
-      }
-      return;
-    }
-    if (kpos >= len) {
+  if (kpos >= len) {
 #pragma unroll
-      for (int db = 0; db < NDB; ++db) sum[db] = f32x16{};
-    }
-    const CrossStride &os = which ? a.dvs : a.dks;
-    store_rows<T, D>(lds + wave * AREA, sum, which ? 1.f : a.scale, lane, [&](int i) {
-      return j0 + i < a.M ? row_ptr<T>(which ? a.dv : a.dk, os, b, {(uint32_t)kvh, (uint32_t)(j0 + i)}) : nullptr;
-    });
-  };
-  put(dk, RH == 2 ? rh : 0);
-  if constexpr (RH == 1) put(dv, 1);
+    for (int db = 0; db < NDB; ++db) dk[db] = f32x16{};
+  }
+  const CrossStride &os = rh ? a.dvs : a.dks;
+  store_rows<T, D>(lds + wave * AREA, dk, rh ? 1.f : a.scale, lane, [&](int i) {
+    return j0 + i < a.M ? row_ptr<T>(rh ? a.dv : a.dk, os, b, {(uint32_t)kvh, (uint32_t)(j0 + i)}) : nullptr;
+  });
 }
 
 // Adds the partial sums of the row splits: one thread per key, gradient and four columns.
@@ -952,8 +957,9 @@ __global__ void __launch_bounds__(256) cross_sum(CrossArgs a) {
   if (j < len) {
     const int splits = splits_of(a, tiles), piece = (before + kvh * per_head) * splits + (j >> a.kshift);
     const float *p = a.part + ((((int64_t)piece << a.kshift) + (j & ((1 << a.kshift) - 1))) * 2 + which) * D + c;
-    for (int s = 0; s < splits; ++s)
-      sum += *reinterpret_cast<const f32x4 *>(p + ((int64_t)(s * per_head) << a.kshift) * 2 * D);
+    const int64_t step = ((int64_t)per_head << a.kshift) * 2 * D;
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4 *>(p + s * step);
   }
   const CrossStride &os = which ? a.dvs : a.dks;
   T *dst = row_ptr<T>(which ? a.dv : a.dk, os, b, {(uint32_t)kvh, (uint32_t)j});
@@ -968,7 +974,7 @@ bool few_rows(const CrossArgs &a) { return (int64_t)a.B * a.kv * ((a.R + 127) / 
 bool keys_stay(const CrossArgs &a) { return a.M <= 128 && a.R > 32; }
 
 // Blocks of 32 keys of a dk / dv workgroup: four (eight waves, one workgroup per CU)
-// where those fill the CUs, runs of 128 rows included.
+// where those fill the CUs, runs of 128 rows included; two, of four waves, otherwise.
 int kv_blocks(const CrossArgs &a) {
   const int64_t most = (int64_t)a.B * a.kv * ((a.M + 127) / 128) * ((a.R + 127) / 128);
   return a.M > 64 && most >= device_cu_count() ? 4 : 2;
@@ -1025,8 +1031,8 @@ hipError_t bwd(CrossArgs &a, hipStream_t s) {
   if (e != hipSuccess) return e;
   a.uneven = a.lengths && a.B <= 64 && a.pieces && a.pieces < bk * a.n_ktiles * a.splits;
   const dim3 grid = deal_grid(a, a.pieces ? a.pieces : bk * a.n_ktiles);
-  if (a.kshift == 6) hipLaunchKernelGGL((cross_dkdv<T, D, 2, 2, RB>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((cross_dkdv<T, D, 4, 2, RB>), grid, dim3(512), 0, s, a);
+  if (a.kshift == 6) hipLaunchKernelGGL((cross_dkdv<T, D, 2, RB>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((cross_dkdv<T, D, 4, RB>), grid, dim3(512), 0, s, a);
   e = hipGetLastError();
   if (e != hipSuccess || !a.pieces) return e;
   const int64_t n = bk * a.M * 2 * (D / 4);

@@ -550,6 +550,7 @@ __global__ void __launch_bounds__(256) finish_kernel(GemmArgs p, int n) {
   const int row = (int)(i / p.NA);
   const int f = (int)(i - (int64_t)row * p.NA);
   float z[V] = {};
+#pragma unroll 4
   for (int k = 0; k < n; ++k)
 #pragma unroll
     for (int e = 0; e < V; e += 4) {
