@@ -4,7 +4,7 @@
 // with -a in place of a for the way back of a gradient; the other features are copied.
 //
 // Bound by HBM: each row is read and written once. A thread owns one unit of a row -
-// a run of pairs that 16 bytes hold, or as many to copy - at one position, computes the
+// the pairs of a 16-byte access or two, or features to copy - at one position, computes the
 // unit's sines and cosines once, and goes through a run of (batch, head) slices with
 // them, so the trigonometry (about 60 operations per pair) is shared. The runs leave the
 // chip 32 waves per CU, two slices' loads in flight each. Measured: 64x64 layer, 6 heads
@@ -16,7 +16,7 @@
 // The angle is formed in float64 and reduced to a fraction of a turn before it is
 // rounded: at position 10^5 and frequency 1 the float32 product is already 4e-3 off,
 // while this is below 2e-7 up to 2^28.
-#include <type_traits>
+#include <algorithm>
 
 #include "attn_common.h"
 
@@ -37,10 +37,62 @@ __device__ __forceinline__ void turn_of(double c, double f, const RopeArgs &p, f
   sn = s * (p.inverse ? -p.magnitude : p.magnitude);
 }
 
-// V: elements per access, the most that divide the run of pairs and fit 16 bytes (a
-// run of an odd number of pairs in halves: 1). INTER: interleaved pairs, a unit is one
-// access; else a unit of pairs is an access to the first half and its partner in the
-// second.
+// The run of slices that a thread goes through with its sines and cosines: slice s is head
+// s % HT of batch element s / HT (q's heads first, then k's). Per-batch positions: a group
+// lies in one batch element.
+struct Slices {
+  int s0, s1, b, h, HT;
+  __device__ __forceinline__ Slices(const RopeArgs &p, uint32_t grp) {
+    HT = p.heads[0] + p.heads[1];
+    if (p.pos_stride) {
+      b = (int)(grp / (uint32_t)p.groups);
+      const int g = (int)grp - b * p.groups;
+      s0 = b * HT + g * p.run;
+      s1 = min(s0 + p.run, (b + 1) * HT);
+    } else {
+      s0 = (int)grp * p.run;
+      s1 = min(s0 + p.run, p.B * HT);
+      b = s0 / HT;
+    }
+    h = s0 - b * HT;
+  }
+  // Row n's position, as (row, column) on a grid.
+  __device__ __forceinline__ void position(const RopeArgs &p, int n, int &r, int &c) const {
+    r = p.pos ? p.pos[(int64_t)(p.pos_stride ? b : 0) * p.pos_stride + n] : n;
+    c = 0;
+    if (p.axes == 2) {
+      const int pos = r;
+      r = (int)((uint32_t)pos / (uint32_t)p.grid_w);
+      c = pos - r * p.grid_w;
+    }
+  }
+  // Row n of the next m slices.
+  template <typename T>
+  __device__ __forceinline__ void rows(const RopeArgs &p, int m, int n, const T *(&src)[kBatch], T *(&dst)[kBatch]) {
+    auto at = [&](const RopeTensor &t, int hh) { return (int64_t)b * t.batch + (int64_t)hh * t.head + (int64_t)n * t.row; };
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      if (j >= m) break;
+      const int k = h >= p.heads[0], hh = h - (k ? p.heads[0] : 0);
+      src[j] = static_cast<const T *>(k ? p.in[1].ptr : p.in[0].ptr) + (k ? at(p.in[1], hh) : at(p.in[0], hh));
+      dst[j] = static_cast<T *>(k ? p.out[1].ptr : p.out[0].ptr) + (k ? at(p.out[1], hh) : at(p.out[0], hh));
+      if (++h == HT) {
+        h = 0;
+        ++b;
+      }
+    }
+  }
+};
+
+template <bool THROUGH, typename T, typename W>
+__device__ __forceinline__ void rope_put(T *q, const W &v) {
+  if constexpr (THROUGH) __builtin_nontemporal_store(v, reinterpret_cast<W *>(q));
+  else *reinterpret_cast<W *>(q) = v;
+}
+
+// V: elements per access. INTER: interleaved pairs, a unit is one access; else a unit of
+// pairs is an access to the first half and its partner in the second, and V divides the
+// run of pairs.
 template <typename T, int V, bool INTER, bool THROUGH>
 __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
   constexpr int VT = V == 1 ? 2 : V;      // elements of a unit to copy (their number is even)
@@ -54,21 +106,8 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
   const uint32_t grp = fdiv(rows, p.n_div);
   const int n = (int)(rows - grp * p.n_div.div);
 
-  // The slices [s0, s1) of this thread: slice s is head s % HT of batch element s / HT
-  // (q's heads first, then k's). Per-batch positions: a group lies in one batch element.
-  const int HT = p.heads[0] + p.heads[1];
-  int s0, s1, b;
-  if (p.pos_stride) {
-    b = (int)(grp / (uint32_t)p.groups);
-    const int g = (int)grp - b * p.groups;
-    s0 = b * HT + g * p.run;
-    s1 = min(s0 + p.run, (b + 1) * HT);
-  } else {
-    s0 = (int)grp * p.run;
-    s1 = min(s0 + p.run, p.B * HT);
-    b = s0 / HT;
-  }
-  int h = s0 - b * HT;
+  Slices sl(p, grp);
+  const int s0 = sl.s0, s1 = sl.s1;
 
   // The unit's features (from e0 on, and from e1 on for the partners) and its first pair.
   const int P = p.pairs, rot = 2 * P * p.axes;
@@ -87,48 +126,29 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
     }
   }
 
+  const int np = P * p.axes - pair;   // (interleaved: the pairs of the unit that are turned)
   float cs[NP], sn[NP];
   if (turned) {
-    const int pos = p.pos ? p.pos[(int64_t)(p.pos_stride ? b : 0) * p.pos_stride + n] : n;
-    int r = pos, c = 0;
-    if (p.axes == 2) {
-      r = (int)((uint32_t)pos / (uint32_t)p.grid_w);
-      c = pos - r * p.grid_w;
-    }
+    int r, c;
+    sl.position(p, n, r, c);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       int pi = pair + i, ax = axis;
-      if (INTER && pi >= P) {   // (a unit may cross from the row's pairs to the column's)
-        pi -= P;
+      if (INTER && pi >= P) {   // (a unit may cross from the row's pairs to the column's, and to features to copy)
+        pi = i < np ? pi - P : 0;
         ax = 1;
       }
       turn_of((double)(ax ? c : r), p.freqs[pi], p, cs[i], sn[i]);
     }
   }
 
-  auto at = [&](const RopeTensor &t, int hh, int bb) { return (int64_t)bb * t.batch + (int64_t)hh * t.head + (int64_t)n * t.row; };
   // Batches of slices: all loads first, then the turns and the stores.
   for (int s = s0; s < s1; s += kBatch) {
     const T *src[kBatch];
     T *dst[kBatch];
     const int m = min(kBatch, s1 - s);
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      if (j >= m) break;
-      const int k = h >= p.heads[0];
-      const int hh = h - (k ? p.heads[0] : 0);
-      src[j] = static_cast<const T *>(k ? p.in[1].ptr : p.in[0].ptr) + (k ? at(p.in[1], hh, b) : at(p.in[0], hh, b));
-      dst[j] = static_cast<T *>(k ? p.out[1].ptr : p.out[0].ptr) + (k ? at(p.out[1], hh, b) : at(p.out[0], hh, b));
-      if (++h == HT) {
-        h = 0;
-        ++b;
-      }
-    }
-    auto put = [](T *q, const auto &v) {
-      using W = std::remove_const_t<std::remove_reference_t<decltype(v)>>;
-      if constexpr (THROUGH) __builtin_nontemporal_store(v, reinterpret_cast<W *>(q));
-      else *reinterpret_cast<W *>(q) = v;
-    };
+    sl.rows(p, m, n, src, dst);
+    auto put = [](T *q, const auto &v) { rope_put<THROUGH>(q, v); };
     if (!INTER && !turned) {
       tail x[kBatch];
 #pragma unroll
@@ -153,9 +173,10 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
           if constexpr (INTER) {
-            const float x1 = (float)a[j][2 * i], x2 = (float)a[j][2 * i + 1];
-            a[j][2 * i] = (T)(x1 * cs[i] - x2 * sn[i]);
-            a[j][2 * i + 1] = (T)(x2 * cs[i] + x1 * sn[i]);
+            const T t1 = a[j][2 * i], t2 = a[j][2 * i + 1];
+            const float x1 = (float)t1, x2 = (float)t2;
+            a[j][2 * i] = i < np ? (T)(x1 * cs[i] - x2 * sn[i]) : t1;
+            a[j][2 * i + 1] = i < np ? (T)(x2 * cs[i] + x1 * sn[i]) : t2;
           } else {
             const float x1 = (float)a[j][i], x2 = (float)c[j][i];
             a[j][i] = (T)(x1 * cs[i] - x2 * sn[i]);
@@ -169,43 +190,125 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
   }
 }
 
+// Halves whose pairs do not fill accesses: a thread owns a 16-byte chunk of a row, and
+// finds its features' partners where the row's other chunks, held by the same wave, have
+// put them in LDS. Features to copy stay as they are. 12 slices of 44540 rows of 64, bf16,
+// 26 pairs on a grid: 31 us (4.4 TB/s); as units of one pair, 2 bytes an access, 58.
+template <typename T, bool THROUGH>
+__global__ void __launch_bounds__(kThreads) rope_chunks(RopeArgs p) {
+  constexpr int V = 16 / (int)sizeof(T);
+  typedef T vec __attribute__((ext_vector_type(V)));
+  __shared__ vec lds[kBatch][kThreads];
+  const int lane = threadIdx.x & 63, per = p.d / V, rows = 64 / per;   // chunks of a row, rows of a wave
+  const int rr = lane / per, u = lane - rr * per;
+  const uint32_t wave = blockIdx.x * (uint32_t)(kThreads / 64) + (threadIdx.x >> 6);
+  const uint32_t grp = fdiv(wave, p.unit_div);
+  const int n = (int)(wave - grp * p.unit_div.div) * rows + rr;
+  if (grp >= p.total || rr >= rows || n >= p.N) return;
+  Slices sl(p, grp);
+
+  const int P = p.pairs, rot = 2 * P * p.axes;
+  float cs[V], sn[V];
+  int other[V];   // the partner's place in the wave's part of LDS, in elements
+  {
+    double freq[V], at[V];   // (all frequencies in flight at once)
+    int r, c;
+    sl.position(p, n, r, c);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int f = u * V + i, axis = f >= 2 * P ? 1 : 0, in = f - axis * 2 * P;
+      const bool first = in < P, turns = f < rot;
+      freq[i] = p.freqs[turns ? (first ? in : in - P) : 0];
+      at[i] = (double)(axis ? c : r);
+      sn[i] = first ? -1.f : 1.f;
+      other[i] = lane * V + i + (turns ? (first ? P : -P) : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      float s;
+      turn_of(at[i], freq[i], p, cs[i], s);
+      sn[i] *= s;
+    }
+  }
+  const int turned = rot - u * V;
+  for (int s = sl.s0; s < sl.s1; s += kBatch) {
+    const T *src[kBatch];
+    T *dst[kBatch];
+    const int m = min(kBatch, sl.s1 - s);
+    sl.rows(p, m, n, src, dst);
+    vec a[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j)
+      if (j < m) a[j] = *reinterpret_cast<const vec *>(src[j] + u * V);
+    // (a wave's LDS operations are in order, so it needs no barrier)
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j)
+      if (j < m) lds[j][threadIdx.x] = a[j];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      if (j >= m) break;
+      const T *part = reinterpret_cast<const T *>(&lds[j][threadIdx.x & ~63]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const T x = a[j][i];
+        const float y = (float)part[other[i]];
+        a[j][i] = i < turned ? (T)((float)x * cs[i] + y * sn[i]) : x;
+      }
+      rope_put<THROUGH>(dst[j] + u * V, a[j]);
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
+// Shares `work` threads per slice out; returns how many groups of slices there are.
+int64_t share_slices(RopeArgs &p, int64_t work) {
+  const int64_t HT = p.heads[0] + p.heads[1], want = (int64_t)device_cu_count() * 2048;
+  const int64_t most = p.pos_stride ? HT : HT * p.B;
+  const int64_t run = std::max<int64_t>(1, std::min(work * HT * p.B / want, most));
+  p.run = (int32_t)run;
+  p.groups = (int32_t)((most + run - 1) / run);
+  return (int64_t)p.groups * (p.pos_stride ? p.B : 1);
+}
+// A call that moves more than the caches hold.
+bool goes_through(const RopeArgs &p, int es) {
+  return 2 * p.B * (int64_t)(p.heads[0] + p.heads[1]) * p.N * p.d * es > (256LL << 20);
+}
+
 template <typename T, int V, bool INTER>
 hipError_t launch(RopeArgs &p, hipStream_t s) {
   const int rot = 2 * p.pairs * p.axes;
   const int units = INTER ? p.d / V : rot / (2 * V) + (p.d - rot) / (V == 1 ? 2 : V);
   p.unit_div = make_fastdiv((uint32_t)units);
   p.n_div = make_fastdiv((uint32_t)p.N);
-  const int64_t per_slice = (int64_t)units * p.N, HT = p.heads[0] + p.heads[1];
-  const int64_t want = (int64_t)device_cu_count() * 2048;
-  int64_t run = per_slice * HT * p.B / want;
-  const int64_t most = p.pos_stride ? HT : HT * p.B;
-  run = run < 1 ? 1 : (run > most ? most : run);
-  p.run = (int32_t)run;
-  p.groups = (int32_t)((most + run - 1) / run);
-  const int64_t total = per_slice * p.groups * (p.pos_stride ? p.B : 1);
+  const int64_t per_slice = (int64_t)units * p.N, total = per_slice * share_slices(p, per_slice);
   p.total = (uint32_t)total;
   const dim3 grid((uint32_t)((total + kThreads - 1) / kThreads));
-  const int64_t bytes = 2 * p.B * HT * p.N * p.d * (int64_t)sizeof(T);
-  if (bytes > (256LL << 20)) hipLaunchKernelGGL((rope_kernel<T, V, INTER, true>), grid, dim3(kThreads), 0, s, p);
+  if (goes_through(p, sizeof(T))) hipLaunchKernelGGL((rope_kernel<T, V, INTER, true>), grid, dim3(kThreads), 0, s, p);
   else hipLaunchKernelGGL((rope_kernel<T, V, INTER, false>), grid, dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
 
-// The widest access that divides the features of an axis' pairs (interleaved) or the
-// pairs themselves.
+template <typename T>
+hipError_t launch_chunks(RopeArgs &p, hipStream_t s) {
+  const int rows = 64 / (p.d * (int)sizeof(T) / 16);
+  const int64_t waves = (p.N + rows - 1) / rows, groups = share_slices(p, 64 * waves);
+  p.unit_div = make_fastdiv((uint32_t)waves);
+  p.total = (uint32_t)groups;
+  constexpr int PER = kThreads / 64;
+  const dim3 grid((uint32_t)((waves * groups + PER - 1) / PER));
+  if (goes_through(p, sizeof(T))) hipLaunchKernelGGL((rope_chunks<T, true>), grid, dim3(kThreads), 0, s, p);
+  else hipLaunchKernelGGL((rope_chunks<T, false>), grid, dim3(kThreads), 0, s, p);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_any(RopeArgs &p, hipStream_t s) {
   constexpr int V = 16 / (int)sizeof(T);
-  if (p.interleaved) {
-    const int n = 2 * p.pairs * p.axes;
-    if (n % V == 0) return launch<T, V, true>(p, s);
-    if (V == 8 && n % 4 == 0) return launch<T, 4, true>(p, s);
-    return launch<T, 2, true>(p, s);
-  }
+  if (p.interleaved) return launch<T, V, true>(p, s);
   if (p.pairs % V == 0) return launch<T, V, false>(p, s);
-  if (V == 8 && p.pairs % 4 == 0) return launch<T, 4, false>(p, s);
-  if (p.pairs % 2 == 0) return launch<T, 2, false>(p, s);
-  return launch<T, 1, false>(p, s);
+  if (p.d <= 64 * V) return launch_chunks<T>(p, s);
+  return launch<T, 1, false>(p, s);   // (rows of over 1 KiB)
 }
 
 }  // namespace

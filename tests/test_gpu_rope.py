@@ -114,6 +114,35 @@ def test_views_of_one_tensor_in_place(interleaved):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,pairs", [(256, 13), (512, 13), (520, 13), (1040, 6), (1040, 260)])
+def test_long_rows(d, pairs, interleaved, dtype):
+    """Rows of a wave's chunks, one more, and many; what is not turned keeps its bits."""
+    freqs, _ = hla.rope_freqs(pairs)
+    x = normal((2, 2, 37, d), dtype, d)
+    x[0, 1, 5, 2 * pairs:2 * pairs + 3] = torch.tensor([float("nan"), float("inf"), -0.0])
+    got = hla.rope(x, freqs, interleaved=interleaved)
+    bits = torch.int16 if dtype is torch.bfloat16 else torch.int32
+    assert torch.equal(got[..., 2 * pairs:].contiguous().view(bits), x[..., 2 * pairs:].contiguous().view(bits))
+    check(got[..., :2 * pairs].contiguous(), x[..., :2 * pairs].contiguous(), freqs, interleaved=interleaved)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_infinity_stays_in_its_pair(interleaved):
+    freqs, _ = hla.rope_freqs(5)
+    x = normal((1, 2, 30, 32), torch.bfloat16, 13)
+    want = hla.rope(x, freqs, interleaved=interleaved)
+    x[0, 1, 7, 3] = float("inf")
+    got = hla.rope(x, freqs, interleaved=interleaved)
+    pair = [2, 3] if interleaved else [3, 8]
+    assert not bool(got[0, 1, 7, pair].isfinite().any())
+    got[0, 1, 7, pair] = want[0, 1, 7, pair]
+    assert torch.equal(got, want)
+
+
+@pytest.mark.gpu
 def test_one_row_for_the_whole_batch():
     freqs, _ = hla.rope_freqs(16)
     x = normal((1, 2, 5, 32), torch.float32, 4)
