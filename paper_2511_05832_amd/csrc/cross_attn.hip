@@ -936,11 +936,14 @@ __global__ void __launch_bounds__(128 * KB, 2) cross_dkdv(CrossArgs a) {
   });
 }
 
-// Adds the partial sums of the row splits: one thread per key, gradient and four columns.
+// Adds the partial sums of the row splits: one thread per key, gradient and four columns,
+// or a.ways of them where there are few keys of many splits, added through LDS in order.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) cross_sum(CrossArgs a) {
   constexpr int TPR = D / 4;
-  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x, keys = (int64_t)a.B * a.kv * a.M;
+  __shared__ f32x4 lds[256];
+  const int lanes = 256 / a.ways, way = (int)threadIdx.x / lanes, slot = (int)threadIdx.x - way * lanes;
+  const int64_t idx = (int64_t)blockIdx.x * lanes + slot, keys = (int64_t)a.B * a.kv * a.M;
   const int c = (int)(idx % TPR) * 4, which = (int)(idx / TPR % 2);
   const int64_t key = min(idx / (2 * TPR), keys - 1);   // (every lane takes part in the scan)
   const int bk = (int)(key / a.M), j = (int)(key - (int64_t)bk * a.M), b = bk / a.kv, kvh = bk - b * a.kv;
@@ -952,15 +955,21 @@ __global__ void __launch_bounds__(256) cross_sum(CrossArgs a) {
     per_head = tiles_of(a, len);
     before = __shfl(kt.before, b);
   }
-  if (idx / (2 * TPR) >= keys) return;
   f32x4 sum = {};
   if (j < len) {
     const int splits = splits_of(a, tiles), piece = (before + kvh * per_head) * splits + (j >> a.kshift);
     const float *p = a.part + ((((int64_t)piece << a.kshift) + (j & ((1 << a.kshift) - 1))) * 2 + which) * D + c;
     const int64_t step = ((int64_t)per_head << a.kshift) * 2 * D;
 #pragma unroll 8
-    for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4 *>(p + s * step);
+    for (int s = way; s < splits; s += a.ways) sum += *reinterpret_cast<const f32x4 *>(p + s * step);
   }
+  if (a.ways > 1) {
+    lds[threadIdx.x] = sum;
+    __syncthreads();
+    if (way == 0)
+      for (int k = 1; k < a.ways; ++k) sum += lds[slot + k * lanes];
+  }
+  if (way || idx / (2 * TPR) >= keys) return;
   const CrossStride &os = which ? a.dvs : a.dks;
   T *dst = row_ptr<T>(which ? a.dv : a.dk, os, b, {(uint32_t)kvh, (uint32_t)j});
   put4<T>(dst + c, sum * (which ? 1.f : a.scale));
@@ -1036,7 +1045,10 @@ hipError_t bwd(CrossArgs &a, hipStream_t s) {
   e = hipGetLastError();
   if (e != hipSuccess || !a.pieces) return e;
   const int64_t n = bk * a.M * 2 * (D / 4);
-  hipLaunchKernelGGL((cross_sum<T, D>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, s, a);
+  a.ways = 1;
+  while (a.ways < 16 && a.pieces / (bk * a.n_ktiles) >= 16 * a.ways && n * a.ways < 256 * (int64_t)device_cu_count()) a.ways *= 2;
+  const int lanes = 256 / a.ways;
+  hipLaunchKernelGGL((cross_sum<T, D>), dim3((uint32_t)((n + lanes - 1) / lanes)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -212,8 +212,9 @@ struct CrossArgs {
   // (backward); workgroups that share a list's rows where the keys stay in LDS; dk / dv:
   // key tiles of a head, of 2^kshift keys, and workgroups that share the tiles (0: one each)
   int32_t splits, per, row_parts, n_ktiles, kshift, pieces;
-  // set by the launchers: row tiles, pieces of work, run dealt to an XCD, dk / dv splits by lengths
-  int32_t n_rtiles, total, unit, uneven;
+  // set by the launchers: row tiles, pieces of work, run dealt to an XCD; dk / dv: splits by
+  // lengths, threads to a sum
+  int32_t n_rtiles, total, unit, uneven, ways;
   FastDiv ndiv;                // division by N
   float scale, scale_log2;
 };
