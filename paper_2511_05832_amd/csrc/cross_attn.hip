@@ -1081,6 +1081,9 @@ bool cross_fwd_plan(CrossArgs &a, int row_bytes) {
 
 // dk and dv: eight waves per CU where key tiles alone would leave half of the CUs without
 // work, of at least 128 rows each. (Only the device knows the lengths, and so the splits.)
+// Rows of 64 bytes leave registers for sixteen waves, which pays from 1024 rows each on
+// (132 tiles of 128 keys, 6144 rows, heads of 32: the backward 122 -> 91 us; 36 tiles, 4096
+// rows: 31 against 34).
 bool cross_bwd_plan(CrossArgs &a, int row_bytes) {
   a.per = (a.M + BN - 1) / BN * BN;
   share_rows(a, row_bytes);
@@ -1088,7 +1091,9 @@ bool cross_bwd_plan(CrossArgs &a, int row_bytes) {
   a.kshift = kb == 2 ? 6 : 7;
   a.n_ktiles = (a.M + 32 * kb - 1) / (32 * kb);
   a.splits = (a.R + 127) / 128;
-  const int64_t slots = (int64_t)device_cu_count() * (kb == 2 ? 2 : 1), tiles = (int64_t)a.B * a.kv * a.n_ktiles;
+  const int64_t cus = device_cu_count(), tiles = (int64_t)a.B * a.kv * a.n_ktiles;
+  const bool two = kb == 2 || (row_bytes <= 64 && tiles * a.R >= 2048 * cus);
+  const int64_t slots = two ? 2 * cus : cus;
   a.pieces = a.splits > 1 && 2 * tiles <= slots ? (int)std::min(slots, tiles * a.splits) : 0;
   return a.pieces > 0;
 }
