@@ -8,8 +8,8 @@
 // unit's sines and cosines once, and goes through a run of (batch, head) slices with
 // them, so the trigonometry (about 60 operations per pair) is shared. The runs leave the
 // chip 32 waves per CU, two slices' loads in flight each. Measured: 64x64 layer, 6 heads
-// of 32, batch 16, bf16 18 us (5.6 TB/s); 65536 tokens, 8 + 2 heads of 64, fp32 57 us
-// (5.9 TB/s; a copy of 1 GiB 5.1).
+// of 32, batch 16, bf16 18 us (5.6 TB/s); 65536 tokens, 8 + 2 heads of 64, fp32 63 us
+// (5.3 TB/s; a copy of 1 GiB 5.1).
 // Results go past the caches where a call moves more than they hold (256 MB): there
 // 77 -> 57 us, while at 84 MB 16.4 -> 18.4 and the next kernel finds its inputs in memory.
 //
@@ -90,10 +90,10 @@ __device__ __forceinline__ void rope_put(T *q, const W &v) {
   else *reinterpret_cast<W *>(q) = v;
 }
 
-// V: elements per access. INTER: interleaved pairs, a unit is one access; else a unit of
-// pairs is an access to the first half and its partner in the second, and V divides the
-// run of pairs.
-template <typename T, int V, bool INTER, bool THROUGH>
+// V: elements per access. INTER: interleaved pairs, a unit is one access, and with MIXED
+// may hold pairs and features to copy; else a unit of pairs is an access to the first half
+// and its partner in the second, and V divides the run of pairs.
+template <typename T, int V, bool INTER, bool MIXED, bool THROUGH>
 __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
   constexpr int VT = V == 1 ? 2 : V;      // elements of a unit to copy (their number is even)
   typedef T vec __attribute__((ext_vector_type(V)));
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
     for (int i = 0; i < NP; ++i) {
       int pi = pair + i, ax = axis;
       if (INTER && pi >= P) {   // (a unit may cross from the row's pairs to the column's, and to features to copy)
-        pi = i < np ? pi - P : 0;
+        pi = !MIXED || i < np ? pi - P : 0;
         ax = 1;
       }
       turn_of((double)(ax ? c : r), p.freqs[pi], p, cs[i], sn[i]);
@@ -175,8 +175,8 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
           if constexpr (INTER) {
             const T t1 = a[j][2 * i], t2 = a[j][2 * i + 1];
             const float x1 = (float)t1, x2 = (float)t2;
-            a[j][2 * i] = i < np ? (T)(x1 * cs[i] - x2 * sn[i]) : t1;
-            a[j][2 * i + 1] = i < np ? (T)(x2 * cs[i] + x1 * sn[i]) : t2;
+            a[j][2 * i] = !MIXED || i < np ? (T)(x1 * cs[i] - x2 * sn[i]) : t1;
+            a[j][2 * i + 1] = !MIXED || i < np ? (T)(x2 * cs[i] + x1 * sn[i]) : t2;
           } else {
             const float x1 = (float)a[j][i], x2 = (float)c[j][i];
             a[j][i] = (T)(x1 * cs[i] - x2 * sn[i]);
@@ -190,9 +190,9 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
   }
 }
 
-// Halves whose pairs do not fill accesses: a thread owns a 16-byte chunk of a row, and
-// finds its features' partners where the row's other chunks, held by the same wave, have
-// put them in LDS. Features to copy stay as they are. 12 slices of 44540 rows of 64, bf16,
+// Halves by chunks: a thread owns 16 bytes of a row, whatever they hold, and finds its
+// features' partners where the row's other chunks, held by the same wave, have put them
+// in LDS. Features to copy stay as they are. 12 slices of 44540 rows of 64, bf16,
 // 26 pairs on a grid: 31 us (4.4 TB/s); as units of one pair, 2 bytes an access, 58.
 template <typename T, bool THROUGH>
 __global__ void __launch_bounds__(kThreads) rope_chunks(RopeArgs p) {
@@ -275,7 +275,7 @@ bool goes_through(const RopeArgs &p, int es) {
   return 2 * p.B * (int64_t)(p.heads[0] + p.heads[1]) * p.N * p.d * es > (256LL << 20);
 }
 
-template <typename T, int V, bool INTER>
+template <typename T, int V, bool INTER, bool MIXED>
 hipError_t launch(RopeArgs &p, hipStream_t s) {
   const int rot = 2 * p.pairs * p.axes;
   const int units = INTER ? p.d / V : rot / (2 * V) + (p.d - rot) / (V == 1 ? 2 : V);
@@ -284,8 +284,8 @@ hipError_t launch(RopeArgs &p, hipStream_t s) {
   const int64_t per_slice = (int64_t)units * p.N, total = per_slice * share_slices(p, per_slice);
   p.total = (uint32_t)total;
   const dim3 grid((uint32_t)((total + kThreads - 1) / kThreads));
-  if (goes_through(p, sizeof(T))) hipLaunchKernelGGL((rope_kernel<T, V, INTER, true>), grid, dim3(kThreads), 0, s, p);
-  else hipLaunchKernelGGL((rope_kernel<T, V, INTER, false>), grid, dim3(kThreads), 0, s, p);
+  if (goes_through(p, sizeof(T))) hipLaunchKernelGGL((rope_kernel<T, V, INTER, MIXED, true>), grid, dim3(kThreads), 0, s, p);
+  else hipLaunchKernelGGL((rope_kernel<T, V, INTER, MIXED, false>), grid, dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
 
@@ -305,10 +305,13 @@ hipError_t launch_chunks(RopeArgs &p, hipStream_t s) {
 template <typename T>
 hipError_t launch_any(RopeArgs &p, hipStream_t s) {
   constexpr int V = 16 / (int)sizeof(T);
-  if (p.interleaved) return launch<T, V, true>(p, s);
-  if (p.pairs % V == 0) return launch<T, V, false>(p, s);
-  if (p.d <= 64 * V) return launch_chunks<T>(p, s);
-  return launch<T, 1, false>(p, s);   // (rows of over 1 KiB)
+  if (p.interleaved) return 2 * p.pairs * p.axes % V ? launch<T, V, true, true>(p, s) : launch<T, V, true, false>(p, s);
+  // Halves: the chunks for rows that a wave holds (up to 1 KiB), but for bf16 pairs that
+  // fill accesses, where both take the same time on many rows and the chunks, whose
+  // threads turn every feature, longer on few (65536 rows of 10 x 64, 32 turned, fp32: 63
+  // against 70 us; 320 rows of 64, bf16: 7.6 against 3.8).
+  if (p.d <= 64 * V && (V == 4 || p.pairs % V)) return launch_chunks<T>(p, s);
+  return p.pairs % V ? launch<T, 1, false, false>(p, s) : launch<T, V, false, false>(p, s);
 }
 
 }  // namespace
