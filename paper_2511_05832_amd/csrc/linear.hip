@@ -190,7 +190,11 @@ __device__ __forceinline__ void finish(const GemmArgs &p, float (&z)[Type<T>::V]
 }
 
 // Output tiles of TB rows by TA columns by WA x WB waves, a ring of RING stages of KB
-// bytes of every row.
+// bytes of every row, filled by the 16-byte LDS DMA. What bounds it, in 256 x 256 tiles:
+// the matrix cores and the LDS reads that feed them, about alike, then the stores, which
+// one workgroup per CU does not hide. 16384 x 4096 results in bf16: 97 us per 1000
+// contracted elements (1.38 PFLOP/s) and 36 us besides; with bias and gelu 14 to 18 us
+// more, and with the residual and the stored pre-activation 32 (403 MB in all).
 template <typename T, int TA, int TB, int WA, int WB, int KB, int RING>
 struct Shape {
   static constexpr int PITCH = TA + 4;   // floats of a staged output row
@@ -456,7 +460,8 @@ __global__ void __launch_bounds__(64 * kFewWaves) few_kernel(GemmArgs p) {
 }
 
 // dz = dy act'(z) (when `dz` is given), and partial column sums of dz for the bias: a
-// workgroup takes 32 chunks of columns by a run of rows.
+// workgroup takes 32 chunks of columns by a run of rows. Bound by HBM: 16384 x 4096, gelu,
+// bf16 82 us (4.9 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(256) dz_kernel(const T *dy, const T *pre, T *dz, float *sums, int T_, int F,
                                                  int rows, int act) {
