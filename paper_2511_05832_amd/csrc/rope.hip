@@ -10,8 +10,9 @@
 // chip 32 waves per CU, two slices' loads in flight each. Measured: 64x64 layer, 6 heads
 // of 32, batch 16, bf16 18 us (5.6 TB/s); 65536 tokens, 8 + 2 heads of 64, fp32 63 us
 // (5.3 TB/s; a copy of 1 GiB 5.1).
-// Results go past the caches where a call moves more than they hold (256 MB): there
-// 77 -> 57 us, while at 84 MB 16.4 -> 18.4 and the next kernel finds its inputs in memory.
+// Results go past the caches where a call moves more than they hold (256 MB; the fp32
+// case 65.9 -> 64.7 us, the units' kernel 77 -> 70), while at 84 MB 16.4 -> 18.4 and the
+// next kernel would find its inputs in memory.
 //
 // The angle is formed in float64 and reduced to a fraction of a turn before it is
 // rounded: at position 10^5 and frequency 1 the float32 product is already 4e-3 off,
@@ -289,10 +290,15 @@ hipError_t launch(RopeArgs &p, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Waves that hold the N rows of a slice (rows of up to 1 KiB).
+int64_t chunk_waves(const RopeArgs &p, int es) {
+  const int rows = 64 / (p.d * es / 16);
+  return (p.N + rows - 1) / rows;
+}
+
 template <typename T>
 hipError_t launch_chunks(RopeArgs &p, hipStream_t s) {
-  const int rows = 64 / (p.d * (int)sizeof(T) / 16);
-  const int64_t waves = (p.N + rows - 1) / rows, groups = share_slices(p, 64 * waves);
+  const int64_t waves = chunk_waves(p, sizeof(T)), groups = share_slices(p, 64 * waves);
   p.unit_div = make_fastdiv((uint32_t)waves);
   p.total = (uint32_t)groups;
   constexpr int PER = kThreads / 64;
@@ -310,7 +316,9 @@ hipError_t launch_any(RopeArgs &p, hipStream_t s) {
   // fill accesses, where both take the same time on many rows and the chunks, whose
   // threads turn every feature, longer on few (65536 rows of 10 x 64, 32 turned, fp32: 63
   // against 70 us; 320 rows of 64, bf16: 7.6 against 3.8).
-  if (p.d <= 64 * V && (V == 4 || p.pairs % V)) return launch_chunks<T>(p, s);
+  // (A batch of short rows with positions of their own may need more waves than a launch has.)
+  if (p.d <= 64 * V && (V == 4 || p.pairs % V) && 64 * chunk_waves(p, sizeof(T)) * (p.pos_stride ? p.B : 1) < (1LL << 31))
+    return launch_chunks<T>(p, s);
   return p.pairs % V ? launch<T, 1, false, false>(p, s) : launch<T, V, false, false>(p, s);
 }
 
