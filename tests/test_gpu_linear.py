@@ -7,7 +7,7 @@ a step of the result's type:
   pre   E_z + h |z|
   y     1.13 E_z + 1e-6 |z| + (h + u) (|act| + |residual|)
         (slopes of the activations stay below 1.13; the bf16 kernel's normal distribution
-        is within 1.5e-7, every exponential and reciprocal within 4 u)
+        is within 3.1e-7, every exponential and reciprocal within 4 u)
   dz    |dy| 2e-6 (1 + |z|) + h |dz|                 z is the pre of the forward
         (rounded for the products; with no activation dz is dy, exact)
   dx    sum_f (E_dz + (F + 3) u |dz|) |w| + h |dx|
