@@ -460,11 +460,12 @@ __global__ void __launch_bounds__(64 * kFewWaves) few_kernel(GemmArgs p) {
 }
 
 // dz = dy act'(z) (when `dz` is given), and partial column sums of dz for the bias: a
-// workgroup takes 32 chunks of columns by a run of rows. Bound by HBM: 16384 x 4096, gelu,
-// bf16 82 us (4.9 TB/s).
+// workgroup takes 32 chunks of columns by a run of rows. Where one run holds them all the
+// sums are the bias' gradient itself (`db`), which saves the adding launch. Bound by HBM:
+// 16384 x 4096, gelu, bf16 82 us (4.9 TB/s).
 template <typename T>
-__global__ void __launch_bounds__(256) dz_kernel(const T *dy, const T *pre, T *dz, float *sums, int T_, int F,
-                                                 int rows, int act) {
+__global__ void __launch_bounds__(256) dz_kernel(const T *dy, const T *pre, T *dz, float *sums, T *db, int T_,
+                                                 int F, int rows, int act) {
   constexpr int V = Type<T>::V;
   typedef T vec __attribute__((ext_vector_type(V)));
   __shared__ float part[8][32 * V];
@@ -496,7 +497,7 @@ __global__ void __launch_bounds__(256) dz_kernel(const T *dy, const T *pre, T *d
       }
     }
   }
-  if (!sums) return;
+  if (!sums && !db) return;
 #pragma unroll
   for (int e = 0; e < V; ++e) part[ry][cx * V + e] = s[e];
   __syncthreads();
@@ -505,7 +506,9 @@ __global__ void __launch_bounds__(256) dz_kernel(const T *dy, const T *pre, T *d
     float t = 0.f;
 #pragma unroll
     for (int y = 0; y < 8; ++y) t += part[y][i];
-    if (f < F) sums[(int64_t)blockIdx.y * F + f] = t;
+    if (f >= F) continue;
+    if (db) db[f] = (T)t;
+    else sums[(int64_t)blockIdx.y * F + f] = t;
   }
 }
 
@@ -710,9 +713,19 @@ hipError_t fwd(const LinearArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Runs of rows of the dz launch: workgroups for every CU four times over.
-int dz_rows(const LinearArgs &a, int V) {
-  const int64_t cols = (a.F / V + 31) / 32;
+// dx [T, K] over F, and dW [F, K] over T.
+template <typename T>
+Plan dx_plan(const LinearArgs &a) { return plan_of<T>(a.K, a.T, a.F, false, true); }
+template <typename T>
+Plan dw_plan(const LinearArgs &a) { return plan_of<T>(a.K, a.F, a.T, false, true); }
+
+// Rows of a run of the dz launch: workgroups for every CU four times over; all of up to 128
+// where no product is in parts, so that there is nothing to add (128 tokens, 800 -> 312,
+// bf16, with the bias: the host issues the backward in 17 us, not 20).
+template <typename T>
+int dz_rows(const LinearArgs &a) {
+  if (a.T <= 128 && dx_plan<T>(a).splits == 1 && dw_plan<T>(a).splits == 1) return a.T;
+  const int64_t cols = (a.F / Type<T>::V + 31) / 32;
   const int64_t runs = std::max<int64_t>(1, std::min<int64_t>((a.T + 31) / 32, 4 * device_cu_count() / cols));
   return (int)((a.T + runs - 1) / runs);
 }
@@ -728,12 +741,13 @@ hipError_t bwd(const LinearArgs &a, hipStream_t s) {
   SumJobs jobs = {};   // dx, dW, db
   hipError_t e;
   if (has_act || a.db) {
-    const int rows = dz_rows(a, V);
+    const int rows = dz_rows<T>(a);
     const dim3 grid((uint32_t)((a.F / V + 31) / 32), (uint32_t)((a.T + rows - 1) / rows));
     hipLaunchKernelGGL((dz_kernel<T>), grid, dim3(256), 0, s, static_cast<const T *>(a.dy), static_cast<const T *>(a.pre),
-                       has_act ? dz : nullptr, a.db ? sums : nullptr, a.T, a.F, rows, a.act);
+                       has_act ? dz : nullptr, a.db && grid.y > 1 ? sums : nullptr,
+                       a.db && grid.y == 1 ? static_cast<T *>(a.db) : nullptr, a.T, a.F, rows, a.act);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (a.db) jobs.job[2] = sum_job(sums, a.db, a.F, (int)grid.y);
+    if (a.db && grid.y > 1) jobs.job[2] = sum_job(sums, a.db, a.F, (int)grid.y);
   }
   const void *g = has_act ? static_cast<const void *>(dz) : a.dy;
   GemmArgs x = {}, w = {};
@@ -749,7 +763,7 @@ hipError_t bwd(const LinearArgs &a, hipStream_t s) {
   w.a = a.x;
   w.out = a.dw;
   w.part = reinterpret_cast<float *>(work + at.dw);
-  const Plan px = plan_of<T>(x.NA, x.NB, x.KC, false, true), pw = plan_of<T>(w.NA, w.NB, w.KC, false, true);
+  const Plan px = dx_plan<T>(a), pw = dw_plan<T>(a);
   if (a.dx && a.dw && px.tile == 64 && pw.tile == 64) {
     if (px.splits > 1) jobs.job[0] = sum_job(x.part, x.out, (int64_t)x.NB * x.NA, px.splits);
     else x.part = nullptr;
@@ -779,9 +793,9 @@ LinearWork work_of(const LinearArgs &a) {
   LinearWork w;
   w.dz = 0;
   w.dx = a.act != HLA_ACT_NONE ? up((int64_t)a.T * a.F * sizeof(T)) : 0;
-  w.dw = w.dx + (a.dx ? up(parts(plan_of<T>(a.K, a.T, a.F, false, true), (int64_t)a.T * a.K)) : 0);
-  w.sums = w.dw + (a.dw ? up(parts(plan_of<T>(a.K, a.F, a.T, false, true), (int64_t)a.F * a.K)) : 0);
-  const int rows = dz_rows(a, Type<T>::V);
+  w.dw = w.dx + (a.dx ? up(parts(dx_plan<T>(a), (int64_t)a.T * a.K)) : 0);
+  w.sums = w.dw + (a.dw ? up(parts(dw_plan<T>(a), (int64_t)a.F * a.K)) : 0);
+  const int rows = dz_rows<T>(a);
   w.bytes = w.sums + (a.db ? up((int64_t)((a.T + rows - 1) / rows) * a.F * 4) : 0);
   return w;
 }
