@@ -181,7 +181,7 @@ hla_status cross_sizes(int64_t B, int64_t heads, int64_t kv_heads, int64_t N, in
   a->Rp = (int32_t)((R + 127) / 128 * 128);
   a->ndiv = make_fastdiv((uint32_t)N);
   const int row_bytes = (int)(d * dtype_size(dtype));
-  const bool parts = backward ? cross_bwd_plan(*a, row_bytes) : cross_fwd_plan(*a, row_bytes);
+  const bool parts = backward ? cross_bwd_plan(*a, (int)d, (int)dtype_size(dtype)) : cross_fwd_plan(*a, row_bytes);
   *bytes = backward ? 8 * bk * a->Rp + (parts ? ((int64_t)a->pieces << a->kshift) * 8 * d : 0)
                     : (parts ? bk * a->splits * R * (4 * d + 8) : 0);
   return HLA_OK;

@@ -1081,10 +1081,14 @@ bool cross_fwd_plan(CrossArgs &a, int row_bytes) {
 
 // dk and dv: eight waves per CU where key tiles alone would leave half of the CUs without
 // work, of at least 128 rows each. (Only the device knows the lengths, and so the splits.)
+// Up to 512 rows in bf16 one workgroup takes them all: four steps cost no more than a
+// launch that joins parts (512 rows, 6 heads of 64, 200 keys: the host issues the backward
+// in 20 us, not 23, and a graph runs it in 17.9, not 18.4; 500 rows in fp32: 55, not 33).
 // Rows of 64 bytes leave registers for sixteen waves, which pays from 1024 rows each on
 // (132 tiles of 128 keys, 6144 rows, heads of 32: the backward 122 -> 91 us; 36 tiles, 4096
 // rows: 31 against 34).
-bool cross_bwd_plan(CrossArgs &a, int row_bytes) {
+bool cross_bwd_plan(CrossArgs &a, int d, int es) {
+  const int row_bytes = d * es;
   a.per = (a.M + BN - 1) / BN * BN;
   share_rows(a, row_bytes);
   const int kb = kv_blocks(a);
@@ -1094,7 +1098,7 @@ bool cross_bwd_plan(CrossArgs &a, int row_bytes) {
   const int64_t cus = device_cu_count(), tiles = (int64_t)a.B * a.kv * a.n_ktiles;
   const bool two = kb == 2 || (row_bytes <= 64 && tiles * a.R >= 2048 * cus);
   const int64_t slots = two ? 2 * cus : cus;
-  a.pieces = a.splits > 1 && 2 * tiles <= slots ? (int)std::min(slots, tiles * a.splits) : 0;
+  a.pieces = a.R > (es == 2 ? 512 : 128) && 2 * tiles <= slots ? (int)std::min(slots, tiles * a.splits) : 0;
   return a.pieces > 0;
 }
 

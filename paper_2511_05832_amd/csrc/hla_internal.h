@@ -220,7 +220,7 @@ struct CrossArgs {
 };
 // Share out the work, from B, kv, R and M; true: partial sums go to a workspace.
 bool cross_fwd_plan(CrossArgs &a, int row_bytes);
-bool cross_bwd_plan(CrossArgs &a, int row_bytes);
+bool cross_bwd_plan(CrossArgs &a, int d, int es);
 hipError_t launch_cross_fwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s);
 hipError_t launch_cross_bwd(CrossArgs a, int d, hla_dtype dtype, hipStream_t s);
 
