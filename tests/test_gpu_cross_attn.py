@@ -151,6 +151,30 @@ def test_gradients_of_uneven_lengths(size, lengths, dtype):
 
 
 @pytest.mark.gpu
+def test_replays_with_other_lengths():
+    """A captured step whose lengths change between replays, row splits of dk and dv with them."""
+    q, k, v, dout = inputs(5, 2, 1, 2000, 300, 32, BF, seed=10)
+    n = torch.full((5,), 300, dtype=torch.int32, device="cuda")
+
+    def step():
+        out, lse = hla.cross_attn_fwd(q, k, v, n)
+        return (out, lse, *hla.cross_attn_bwd(q, k, v, out, dout, lse, n))
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for lengths in ([300, 0, 3, 128, 129], [0, 0, 64, 0, 0], [0] * 5, [300] * 5):
+        n.copy_(torch.tensor(lengths, dtype=torch.int32))
+        for t in got:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, want in zip(got, step()):
+            assert torch.equal(t, want), lengths
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("size", [(2, 4, 2, 40, 77, 64), (4, 6, 6, 1, 200, 32)], ids=str)
 def test_views_of_projections(size, dtype):
