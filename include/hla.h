@@ -498,7 +498,8 @@ hla_status hla_rope(const hla_view *q, const hla_view *k, const hla_view *q_out,
  * Any N, M >= 1: few rows (a decoder's single token) against many states split the
  * states over workgroups.
  * out may not overlap q, k, v, lengths or lse. bf16: products on bf16 matrix cores, softmax
- * weights rounded to bf16 as operands, fp32 sums; f32: fp32 throughout.
+ * weights rounded to bf16 as operands, fp32 sums; f32: fp32 throughout. The sums before
+ * the division by a row's weight reach 2^12 M |v|, so |v| above 2^116 / M may overflow.
  * work: device workspace of at least the bytes that hla_cross_attn_workspace gives for
  * these sizes on the current device, 16-byte aligned, overlapping no tensor; may be
  * NULL where that is 0. A call's work is done with it when the call's work is done;

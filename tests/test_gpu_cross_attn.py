@@ -344,6 +344,26 @@ def test_streams_at_once():
         assert torch.equal(t, want[i % 2])
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+# keys that stay in LDS; few rows, without and with key splits; many rows
+@pytest.mark.parametrize("size", [(1, 2, 2, 300, 77, 32), (2, 4, 2, 40, 300, 64), (2, 4, 2, 1, 3000, 64),
+                                  (4, 2, 2, 4001, 321, 64)], ids=str)
+def test_large_values(size, dtype):
+    """Values of 2^101 under scores of 16: the results are in range, and no sum before the
+    division by the row's weight may leave it (weights about a reference of 0, e^16 each,
+    would take 30 of them to 2^129)."""
+    q, k, v, _ = inputs(*size, dtype, seed=21)
+    q, k = 1 + 0.05 * q, 1 + 0.05 * k
+    v = 2.0 ** 101 * v.abs()
+    scale = 16.0 / size[-1]
+    out, lse = hla.cross_attn_fwd(q, k, v, scale=scale)
+    ref = reference(q[:1, :1], k[:1, :1], v[:1, :1], None, scale)
+    compare("out", out[:1, :1], ref)
+    compare("lse", lse[:1, :1], ref)
+    assert bool(out.isfinite().all())
+
+
 class Raw:
     """The C entries on made-up addresses: every call here must be refused."""
     Q, K, V, O, L, W, G, DQ, DK, DV, N = (0x10000000 * i for i in range(1, 12))
