@@ -543,7 +543,8 @@ hla_status hla_cross_attn_workspace(int64_t B, int64_t heads, int64_t kv_heads, 
  * (rounded to dtype), which the backward of an activation needs. residual may be y
  * (the same address); other overlaps of y or pre are INVALID_ARG.
  * HLA_ACT_GELU is z Phi(z); HLA_ACT_GELU_TANH its tanh form, z / 2 (1 + tanh(sqrt(2 /
- * pi) (z + 0.044715 z^3))); HLA_ACT_SILU z / (1 + e^-z).
+ * pi) (z + 0.044715 z^3))); HLA_ACT_SILU z / (1 + e^-z). At z = -inf relu and gelu are 0,
+ * the other two NaN; at -inf and inf the slopes in the backward are their limits.
  * bf16: products on bf16 matrix cores, everything up to y in fp32, rounded once; f32:
  * fp32 throughout.
  * work: device workspace, 16-byte aligned, overlapping no tensor, or NULL. With the bytes

@@ -215,6 +215,29 @@ def test_activations_far_out(act, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("T", [8, 72])
+def test_infinite_arguments(T, act, dtype):
+    """In either type: at inf an activation is inf, at -inf relu and gelu are 0 (the other
+    two NaN), slopes are their limits at both, and NaN stays NaN."""
+    inf, nan = math.inf, math.nan
+    z = torch.tensor([inf, -inf, nan, 1.0] * (T // 4)).to(dtype).cuda()
+    x, w = torch.zeros(T, 8, dtype=dtype, device="cuda"), torch.zeros(8, 8, dtype=dtype, device="cuda")
+    x[:, 0] = z
+    w[:, 0] = 1.0
+    y, pre = hla.linear(x, w, act=act, with_pre=True)
+    assert torch.equal(pre[0::4], torch.full_like(pre[0::4], inf)) and bool(pre[2::4].isnan().all())
+    assert bool((y[0::4] == inf).all()) and bool(y[2::4].isnan().all())
+    assert bool((y[1::4] == 0).all()) if act in ("relu", "gelu") else bool(y[1::4].isnan().all())
+    assert bool(y[3::4].isfinite().all())
+    dx, _, _ = hla.linear_bwd(torch.zeros_like(x), w, torch.ones_like(y), pre, act=act)
+    assert bool((dx[0::4, 0] == 8).all()) and bool((dx[1::4, 0] == 0).all()) and bool(dx[3::4].isfinite().all())
+    if act != "relu":
+        assert bool(dx[2::4, 0].isnan().all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [7, 200])
 def test_nan_and_infinity_stay_in_their_rows(T):
     x, w, b, r, _ = make(T, 72, 40, BF, seed=4)
