@@ -505,8 +505,9 @@ hla_status hla_rope(const hla_view *q, const hla_view *k, const hla_view *q_out,
  * NULL where that is 0. A call's work is done with it when the call's work is done;
  * calls whose work overlaps in time need one each.
  * Supported: d in {32, 64}; row strides of k and v below 2^25 bytes; a batch element of a
- * view within 2^36 bytes; M, heads / kv_heads * N and B * kv_heads up to 2^30, and that
- * times either list of rows up to 2^36; otherwise UNSUPPORTED.
+ * view within 2^36 bytes; M and heads / kv_heads * N up to 2^30; B * kv_heads * M up to
+ * 2^36; B * kv_heads * ceil(heads / kv_heads * N / 128) and, for the backward, 2 * B *
+ * kv_heads * ceil(M / 128) up to 2^24 - 2^9; otherwise UNSUPPORTED.
  */
 hla_status hla_cross_attn_fwd(const hla_view *q, const hla_view *k, const hla_view *v,
                               const int32_t *lengths, const hla_view *out, float *lse, int64_t B,
@@ -552,8 +553,8 @@ hla_status hla_cross_attn_workspace(int64_t B, int64_t heads, int64_t kv_heads, 
  * workgroups where the results alone are too few to fill the GPU; with less it is not,
  * which is slower and sums in another order. Calls whose work overlaps in time need one
  * each.
- * Any T >= 1; K and F multiples of 8 (bf16) or 4 (f32), below 2^20; T up to 2^30,
- * T * max(K, F) up to 2^42; otherwise UNSUPPORTED.
+ * Any T >= 1; K and F multiples of 8 (bf16) or 4 (f32), below 2^20; T up to 2^30; with
+ * each rounded up to 64, T * max(K, F) and K * F up to 2^36 - 2^14; otherwise UNSUPPORTED.
  */
 typedef enum {
   HLA_ACT_NONE = 0,

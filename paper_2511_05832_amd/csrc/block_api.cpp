@@ -155,6 +155,10 @@ CrossStride cross_stride(const ViewShape &s) {
   return {s.v.batch * s.es, (uint32_t)(s.v.head * s.es / 16), (uint32_t)(s.v.row * s.es / 16)};
 }
 
+// A launch counts its threads in 32 bits: below 2^24 workgroups of 256 (of 512, half as
+// many, which are counted twice), the rounding of their number included.
+constexpr int64_t kMostGroups = (1 << 24) - 512;
+
 // Sizes of a cross attention, into the kernel's arguments, and its workspace.
 hla_status cross_sizes(int64_t B, int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d,
                        hla_dtype dtype, bool backward, CrossArgs *a, int64_t *bytes) {
@@ -168,9 +172,9 @@ hla_status cross_sizes(int64_t B, int64_t heads, int64_t kv_heads, int64_t N, in
   if (B > most || heads > most || N > most || M > most || G > most / N || B > most / kv_heads)
     return fail(HLA_ERR_UNSUPPORTED, "heads / kv_heads * N, M or B * kv_heads exceeds 2^30");
   const int64_t bk = B * kv_heads, R = G * N;
-  // (every grid, in workgroups: below 2^31 with 64 rows or keys, or 256 threads, each)
-  if (R > (1LL << 36) / bk || M > (1LL << 36) / bk)
-    return fail(HLA_ERR_UNSUPPORTED, "B * heads * N or B * kv_heads * M exceeds 2^36");
+  if (M > (1LL << 36) / bk) return fail(HLA_ERR_UNSUPPORTED, "B * kv_heads * M exceeds 2^36");
+  if (bk * ((R + 127) / 128) > kMostGroups || (backward && 2 * bk * ((M + 127) / 128) > kMostGroups))
+    return fail(HLA_ERR_UNSUPPORTED, "B * kv_heads times the tiles of 128 rows, or twice those of 128 keys, is not below 2^24 - 2^9");
   a->B = (int32_t)B;
   a->heads = (int32_t)heads;
   a->kv = (int32_t)kv_heads;
@@ -355,8 +359,11 @@ hla_status linear_sizes(int64_t T, int64_t K, int64_t F, hla_act act, hla_dtype 
                 (long long)(16 / es));
   if (T > (1LL << 30) || K >= (1 << 20) || F >= (1 << 20))
     return fail(HLA_ERR_UNSUPPORTED, "T above 2^30, or K or F not below 2^20");
-  // (workgroups of the smallest tiles, and of the 16-feature ones)
-  if (((T + 63) / 64) * ((std::max(K, F) + 63) / 64) > (1LL << 30)) return fail(HLA_ERR_UNSUPPORTED, "T * max(K, F) above 2^42");
+  // (a launch counts its threads in 32 bits: below 2^24 workgroups of 256, one to a tile of
+  // 64 x 64; larger tiles have up to 512 threads, and are at most half as many)
+  const int64_t t = (T + 63) / 64, k = (K + 63) / 64, f = (F + 63) / 64, most = (1 << 24) - 4;
+  if (t * std::max(k, f) > most || k * f > most)
+    return fail(HLA_ERR_UNSUPPORTED, "T * max(K, F) or K * F, in tiles of 64 x 64, is not below 2^36");
   *a = {};
   a->T = (int32_t)T;
   a->K = (int32_t)K;

@@ -445,6 +445,19 @@ def test_refusals_of_overlaps(backward, kw, text):
     assert st == INV and text in msg, (st, msg)
 
 
+def test_more_workgroups_than_a_launch_holds():
+    """A launch counts its threads in 32 bits: 2^24 workgroups of 256 are too many."""
+    for B, kv, N in ((1 << 22, 4, 1), (3 << 20, 4, 129)):
+        for backward in (0, 1):
+            st, msg = Raw()(backward, dict(B=B, heads=kv, kv=kv, N=N, M=1))
+            assert st == UNS and "2^24" in msg, (st, msg)
+    n = ctypes.c_int64()
+    L = hla.lib()
+    for M, want in ((1 << 30, UNS), ((1 << 30) - (1 << 16), hla.HLA_OK)):   # keys of the backward only
+        assert L.hla_cross_attn_workspace(1, 1, 1, 1, M, 64, hla.HLA_BF16, 1, ctypes.byref(n)) == want
+        assert L.hla_cross_attn_workspace(1, 1, 1, 1, M, 64, hla.HLA_BF16, 0, ctypes.byref(n)) == hla.HLA_OK
+
+
 def test_workspace_sizes():
     n = ctypes.c_int64()
     L = hla.lib()

@@ -361,6 +361,18 @@ def test_refusals_backward(kw, status, text):
     assert st == status and text in hla.lib().hla_last_error().decode(), hla.lib().hla_last_error()
 
 
+@pytest.mark.parametrize("T,K,F", [(1 << 30, 8, 8), (1 << 30, 8, 64), (1 << 26, 1024, 8), (1 << 26, 8, 1024),
+                                   (128, (1 << 20) - 8, (1 << 20) - 8)], ids=str)
+@pytest.mark.parametrize("dtype", [hla.HLA_BF16, hla.HLA_F32])
+def test_more_workgroups_than_a_launch_holds(T, K, F, dtype):
+    """A launch counts its threads in 32 bits: 2^24 workgroups of 256 are too many."""
+    n = ctypes.c_int64()
+    for backward in (0, 1):
+        st = hla.lib().hla_linear_workspace(T, K, F, 2, dtype, backward, ctypes.byref(n))
+        assert st == UNS and "2^36" in hla.lib().hla_last_error().decode()
+    assert hla.lib().hla_linear_workspace((1 << 30) - 256, 8, 64, 2, dtype, 1, ctypes.byref(n)) == hla.HLA_OK
+
+
 def test_refusals_of_the_binding():
     x, w = torch.zeros(4, 8), torch.zeros(8, 8)
     with pytest.raises(hla.HLAError, match="GPU"):
