@@ -10,7 +10,8 @@
  *
  * Conventions shared by every entry point
  *  - Every call returns hla_status; HLA_OK is 0. No call throws or aborts.
- *  - Arguments are validated on the host before any HIP call. On a status other
+ *  - Arguments are validated on the host before any HIP call; where a workspace's size
+ *    depends on the device, that is asked for it before the last checks. On a status other
  *    than HLA_OK nothing has been enqueued and no output has been written; the
  *    text of the error is available from hla_last_error() on the same thread.
  *  - Device pointers are plain device addresses owned by the caller. The library

@@ -1,6 +1,7 @@
 // C-ABI entry points of the operators around the attention in a transformer block:
-// argument validation on the host, then launch. As in hla_api.cpp every check runs
-// before the first HIP call.
+// argument validation on the host, then launch. Every check but the workspace's runs before
+// the first HIP call; how large that has to be depends on the device, so the device is asked
+// for its size (nothing else) before those last checks. Nothing is enqueued before all pass.
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
@@ -159,9 +160,9 @@ CrossStride cross_stride(const ViewShape &s) {
 // many, which are counted twice), the rounding of their number included.
 constexpr int64_t kMostGroups = (1 << 24) - 512;
 
-// Sizes of a cross attention, into the kernel's arguments, and its workspace.
+// Sizes of a cross attention, into the kernel's arguments.
 hla_status cross_sizes(int64_t B, int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d,
-                       hla_dtype dtype, bool backward, CrossArgs *a, int64_t *bytes) {
+                       hla_dtype dtype, bool backward, CrossArgs *a) {
   if (!dtype_size(dtype)) return fail(HLA_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
   if (B <= 0 || heads <= 0 || kv_heads <= 0 || N <= 0 || M <= 0 || d <= 0)
     return fail(HLA_ERR_INVALID_ARG, "sizes must be positive");
@@ -184,20 +185,15 @@ hla_status cross_sizes(int64_t B, int64_t heads, int64_t kv_heads, int64_t N, in
   a->R = (int32_t)R;
   a->Rp = (int32_t)((R + 127) / 128 * 128);
   a->ndiv = make_fastdiv((uint32_t)N);
-  const int row_bytes = (int)(d * dtype_size(dtype));
-  const bool parts = backward ? cross_bwd_plan(*a, (int)d, (int)dtype_size(dtype)) : cross_fwd_plan(*a, row_bytes);
-  *bytes = backward ? 8 * bk * a->Rp + (parts ? ((int64_t)a->pieces << a->kshift) * 8 * d : 0)
-                    : (parts ? bk * a->splits * R * (4 * d + 8) : 0);
   return HLA_OK;
 }
 
-hla_status cross_work(int64_t need, const void *work, int64_t bytes) {
-  if (!need) return HLA_OK;
-  if (!work) return fail(HLA_ERR_INVALID_ARG, "work is NULL, %lld bytes are needed", (long long)need);
-  if (!aligned(work, 16)) return fail(HLA_ERR_INVALID_ARG, "work is not 16-byte aligned");
-  if (bytes < need)
-    return fail(HLA_ERR_INVALID_ARG, "work has %lld bytes, %lld are needed", (long long)bytes, (long long)need);
-  return HLA_OK;
+// How the work is shared out on the current device; returns the bytes of workspace.
+int64_t cross_plan(CrossArgs &a, int64_t d, hla_dtype dtype, bool backward) {
+  const int64_t es = dtype_size(dtype), bk = (int64_t)a.B * a.kv;
+  if (!backward) return cross_fwd_plan(a, (int)(d * es)) ? bk * a.splits * a.R * (4 * d + 8) : 0;
+  const bool parts = cross_bwd_plan(a, (int)d, (int)es);
+  return 8 * bk * a.Rp + (parts ? ((int64_t)a.pieces << a.kshift) * 8 * d : 0);
 }
 
 hla_status cross_scale(float scale, CrossArgs *a) {
@@ -213,8 +209,10 @@ struct Range {
   const char *name;
   const void *p;
   int64_t bytes;
+  bool given() const { return p && bytes; }
 };
-hla_status cross_views(ViewShape *t, int n_in, int n, std::initializer_list<Range> ranges) {
+typedef std::initializer_list<Range> Ranges;
+hla_status cross_views(ViewShape *t, int n_in, int n, Ranges ranges) {
   hla_status st;
   for (int i = 0; i < n; ++i)
     if ((st = check_view(t[i], i >= n_in)) != HLA_OK) return st;
@@ -229,8 +227,24 @@ hla_status cross_views(ViewShape *t, int n_in, int n, std::initializer_list<Rang
       if (views_clash(t[i], t[j])) return fail(HLA_ERR_INVALID_ARG, "%s overlaps %s", t[i].name, t[j].name);
   for (const Range &r : ranges)
     for (int i = n_in; i < n; ++i)
-      if (r.p && r.bytes && view_clash(t[i], r.p, r.bytes))
+      if (r.given() && view_clash(t[i], r.p, r.bytes))
         return fail(HLA_ERR_INVALID_ARG, "%s overlaps %s", t[i].name, r.name);
+  return HLA_OK;
+}
+
+// The workspace, which lies on none of them.
+hla_status cross_work(int64_t need, const void *work, int64_t bytes, const ViewShape *t, int n_in, int n, Ranges ranges) {
+  if (!need) return HLA_OK;
+  if (!work) return fail(HLA_ERR_INVALID_ARG, "work is NULL, %lld bytes are needed", (long long)need);
+  if (!aligned(work, 16)) return fail(HLA_ERR_INVALID_ARG, "work is not 16-byte aligned");
+  if (bytes < need)
+    return fail(HLA_ERR_INVALID_ARG, "work has %lld bytes, %lld are needed", (long long)bytes, (long long)need);
+  for (int i = 0; i < n; ++i)
+    if (view_clash(t[i], work, need))
+      return i < n_in ? fail(HLA_ERR_INVALID_ARG, "work overlaps %s", t[i].name)
+                      : fail(HLA_ERR_INVALID_ARG, "%s overlaps work", t[i].name);
+  for (const Range &r : ranges)
+    if (r.given() && overlaps(r.p, r.bytes, work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps %s", r.name);
   return HLA_OK;
 }
 
@@ -243,7 +257,10 @@ hla_status hla_cross_attn_workspace(int64_t B, int64_t heads, int64_t kv_heads, 
                                     int64_t *bytes) {
   CrossArgs a;
   if (!bytes) return fail(HLA_ERR_INVALID_ARG, "bytes is NULL");
-  return cross_sizes(B, heads, kv_heads, N, M, d, dtype, backward != 0, &a, bytes);
+  hla_status st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, backward != 0, &a);
+  if (st != HLA_OK) return st;
+  *bytes = cross_plan(a, d, dtype, backward != 0);
+  return HLA_OK;
 }
 
 hla_status hla_cross_attn_fwd(const hla_view *q, const hla_view *k, const hla_view *v,
@@ -254,24 +271,20 @@ hla_status hla_cross_attn_fwd(const hla_view *q, const hla_view *k, const hla_vi
   hla_status st;
   CrossArgs a = {};
   if (!q || !k || !v || !out) return fail(HLA_ERR_INVALID_ARG, "q, k, v or out is NULL");
-  int64_t need = 0;
-  if ((st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, false, &a, &need)) != HLA_OK) return st;
+  if ((st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, false, &a)) != HLA_OK) return st;
   if ((st = cross_scale(scale, &a)) != HLA_OK) return st;
   if (lse && !aligned(lse, 4)) return fail(HLA_ERR_INVALID_ARG, "lse is not 4-byte aligned");
   if (lengths && !aligned(lengths, 4)) return fail(HLA_ERR_INVALID_ARG, "lengths is not 4-byte aligned");
   const int64_t es = dtype_size(dtype), lse_bytes = lse ? B * heads * N * 4 : 0;
   ViewShape t[4] = {{"q", *q, {B, heads, N}, d, es}, {"k", *k, {B, kv_heads, M}, d, es},
                     {"v", *v, {B, kv_heads, M}, d, es}, {"out", *out, {B, heads, N}, d, es}};
-  if ((st = cross_views(t, 3, 4, {{"lse", lse, lse_bytes}, {"lengths", lengths, B * 4}, {"work", work, need}})) != HLA_OK)
-    return st;
-  if ((st = cross_work(need, work, work_bytes)) != HLA_OK) return st;
-  for (int i = 0; i < 3; ++i) {
-    if (need && view_clash(t[i], work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps %s", t[i].name);
+  const Ranges ranges = {{"lse", lse, lse_bytes}, {"lengths", lengths, B * 4}};
+  if ((st = cross_views(t, 3, 4, ranges)) != HLA_OK) return st;
+  for (int i = 0; i < 3; ++i)
     if (lse && view_clash(t[i], lse, lse_bytes)) return fail(HLA_ERR_INVALID_ARG, "lse overlaps %s", t[i].name);
-  }
-  if (lse && need && overlaps(lse, lse_bytes, work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps lse");
   if (lse && lengths && overlaps(lse, lse_bytes, lengths, B * 4)) return fail(HLA_ERR_INVALID_ARG, "lse overlaps lengths");
-  if (lengths && need && overlaps(lengths, B * 4, work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps lengths");
+  const int64_t need = cross_plan(a, d, dtype, false);
+  if ((st = cross_work(need, work, work_bytes, t, 3, 4, ranges)) != HLA_OK) return st;
   a.q = t[0].v.ptr;
   a.k = t[1].v.ptr;
   a.v = t[2].v.ptr;
@@ -298,8 +311,7 @@ hla_status hla_cross_attn_bwd(const hla_view *q, const hla_view *k, const hla_vi
   hla_status st;
   CrossArgs a = {};
   if (!q || !k || !v || !out || !dout || !dq || !dk || !dv) return fail(HLA_ERR_INVALID_ARG, "a tensor is NULL");
-  int64_t need = 0;
-  if ((st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, true, &a, &need)) != HLA_OK) return st;
+  if ((st = cross_sizes(B, heads, kv_heads, N, M, d, dtype, true, &a)) != HLA_OK) return st;
   if ((st = cross_scale(scale, &a)) != HLA_OK) return st;
   if (!lse) return fail(HLA_ERR_INVALID_ARG, "lse is NULL");
   if (!aligned(lse, 4)) return fail(HLA_ERR_INVALID_ARG, "lse is not 4-byte aligned");
@@ -309,13 +321,10 @@ hla_status hla_cross_attn_bwd(const hla_view *q, const hla_view *k, const hla_vi
                     {"v", *v, {B, kv_heads, M}, d, es},    {"out", *out, {B, heads, N}, d, es},
                     {"dout", *dout, {B, heads, N}, d, es}, {"dq", *dq, {B, heads, N}, d, es},
                     {"dk", *dk, {B, kv_heads, M}, d, es},  {"dv", *dv, {B, kv_heads, M}, d, es}};
-  if ((st = cross_views(t, 5, 8, {{"lse", lse, lse_bytes}, {"lengths", lengths, B * 4}, {"work", work, need}})) != HLA_OK)
-    return st;
-  if ((st = cross_work(need, work, work_bytes)) != HLA_OK) return st;
-  for (int i = 0; i < 5; ++i)
-    if (view_clash(t[i], work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps %s", t[i].name);
-  if (overlaps(lse, lse_bytes, work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps lse");
-  if (lengths && overlaps(lengths, B * 4, work, need)) return fail(HLA_ERR_INVALID_ARG, "work overlaps lengths");
+  const Ranges ranges = {{"lse", lse, lse_bytes}, {"lengths", lengths, B * 4}};
+  if ((st = cross_views(t, 5, 8, ranges)) != HLA_OK) return st;
+  const int64_t need = cross_plan(a, d, dtype, true);
+  if ((st = cross_work(need, work, work_bytes, t, 5, 8, ranges)) != HLA_OK) return st;
   a.q = t[0].v.ptr;
   a.k = t[1].v.ptr;
   a.v = t[2].v.ptr;
@@ -391,6 +400,16 @@ hla_status linear_tensors(const Tensor *in, int ni, const Tensor *out, int no) {
   return HLA_OK;
 }
 
+// The workspace, which lies on none of them.
+hla_status linear_work(const Tensor *in, int ni, const Tensor *out, int no, const void *work, int64_t need) {
+  if (!aligned(work, 16)) return fail(HLA_ERR_INVALID_ARG, "work is not 16-byte aligned");
+  for (const auto &list : {std::make_pair(in, ni), std::make_pair(out, no)})
+    for (int i = 0; i < list.second; ++i)
+      if (list.first[i].p && overlaps(work, need, list.first[i].p, list.first[i].bytes))
+        return fail(HLA_ERR_INVALID_ARG, "work overlaps %s", list.first[i].name);
+  return HLA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -406,11 +425,12 @@ hla_status hla_linear(const void *x, const void *w, const void *bias, const void
   // (residual == y is allowed: each element is read before it is written, by one thread)
   const Tensor in[4] = {{"x", x, T * K * es}, {"w", w, F * K * es}, {"bias", bias, F * es},
                         {"residual", residual == y ? nullptr : residual, T * F * es}};
+  const Tensor out[2] = {{"y", y, T * F * es}, {"pre", pre, T * F * es}};
+  if ((st = linear_tensors(in, 4, out, 2)) != HLA_OK) return st;
   a.parts = true;
   const int64_t need = linear_fwd_work(a, dtype);
   a.parts = need > 0 && work && work_bytes >= need;
-  const Tensor out[3] = {{"y", y, T * F * es}, {"pre", pre, T * F * es}, {"work", a.parts ? work : nullptr, need}};
-  if ((st = linear_tensors(in, 4, out, 3)) != HLA_OK) return st;
+  if (a.parts && (st = linear_work(in, 4, out, 2, work, need)) != HLA_OK) return st;
   a.work = work;
   a.x = x;
   a.w = w;
@@ -453,14 +473,15 @@ hla_status hla_linear_bwd(const void *x, const void *w, const void *pre, const v
   a.dx = dx;
   a.dw = dw;
   a.db = db;
-  const int64_t es = dtype_size(dtype), need = linear_bwd_work(a, dtype).bytes;
+  const int64_t es = dtype_size(dtype);
   const Tensor in[4] = {{"x", x, T * K * es}, {"w", w, F * K * es}, {"pre", pre, T * F * es}, {"dy", dy, T * F * es}};
-  const Tensor out[4] = {{"dx", dx, T * K * es}, {"dw", dw, F * K * es}, {"db", db, F * es},
-                         {"work", need ? work : nullptr, need}};
+  const Tensor out[3] = {{"dx", dx, T * K * es}, {"dw", dw, F * K * es}, {"db", db, F * es}};
+  if ((st = linear_tensors(in, 4, out, 3)) != HLA_OK) return st;
+  const int64_t need = linear_bwd_work(a, dtype).bytes;
   if (need && !work) return fail(HLA_ERR_INVALID_ARG, "work is NULL, %lld bytes are needed", (long long)need);
   if (work_bytes < need)
     return fail(HLA_ERR_INVALID_ARG, "work has %lld bytes, %lld are needed", (long long)work_bytes, (long long)need);
-  if ((st = linear_tensors(in, 4, out, 4)) != HLA_OK) return st;
+  if (need && (st = linear_work(in, 4, out, 3, work, need)) != HLA_OK) return st;
   a.work = work;
   return hip_status(launch_linear_bwd(a, dtype, (hipStream_t)stream), "hla_linear_bwd");
 }

@@ -445,6 +445,18 @@ def test_refusals_of_overlaps(backward, kw, text):
     assert st == INV and text in msg, (st, msg)
 
 
+@pytest.mark.parametrize("backward,kw,text", [
+    (0, dict(q=(Raw.Q + 8, *ROW)), "q is not 16-byte aligned"),
+    (0, dict(out=(Raw.V, *ROW)), "out overlaps v"),
+    (1, dict(dk=(Raw.DQ, *ROW)), "dk overlaps dq"),
+    (1, dict(lse=Raw.DV), "dv overlaps lse"),
+], ids=str)
+def test_tensors_are_checked_before_the_workspace(backward, kw, text):
+    """The size of the workspace depends on the device, which is asked last."""
+    st, msg = Raw()(backward, dict(kw, N=1, M=2048, B=1, heads=1, kv=1, work=0))
+    assert st == INV and text in msg, (st, msg)
+
+
 def test_more_workgroups_than_a_launch_holds():
     """A launch counts its threads in 32 bits: 2^24 workgroups of 256 are too many."""
     for B, kv, N in ((1 << 22, 4, 1), (3 << 20, 4, 129)):

@@ -361,6 +361,14 @@ def test_refusals_backward(kw, status, text):
     assert st == status and text in hla.lib().hla_last_error().decode(), hla.lib().hla_last_error()
 
 
+def test_tensors_are_checked_before_the_workspace():
+    """The size of the workspace depends on the device, which is asked last."""
+    st = hla.lib().hla_linear_bwd(X + 8, W, P, G, 2, DX, DW, DB, 128, 64, 64, hla.HLA_BF16, 0, 0, None)
+    assert st == INV and "x is not 16-byte aligned" in hla.lib().hla_last_error().decode()
+    st = hla.lib().hla_linear_bwd(X, W, P, G, 2, DX, DX, DB, 128, 64, 64, hla.HLA_BF16, 0, 0, None)
+    assert st == INV and "dw overlaps dx" in hla.lib().hla_last_error().decode()
+
+
 @pytest.mark.parametrize("T,K,F", [(1 << 30, 8, 8), (1 << 30, 8, 64), (1 << 26, 1024, 8), (1 << 26, 8, 1024),
                                    (128, (1 << 20) - 8, (1 << 20) - 8)], ids=str)
 @pytest.mark.parametrize("dtype", [hla.HLA_BF16, hla.HLA_F32])
