@@ -38,6 +38,10 @@ __device__ __forceinline__ void turn_of(double c, double f, const RopeArgs &p, f
   sn = s * (p.inverse ? -p.magnitude : p.magnitude);
 }
 
+// x c + y s, y the pair's other member. The order of roundings is written out, so that a row
+// has the same bits in every kernel and in a call of any size.
+__device__ __forceinline__ float turned(float x, float y, float c, float s) { return __builtin_fmaf(x, c, y * s); }
+
 // The run of slices that a thread goes through with its sines and cosines: slice s is head
 // s % HT of batch element s / HT (q's heads first, then k's). Per-batch positions: a group
 // lies in one batch element.
@@ -113,11 +117,11 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
   // The unit's features (from e0 on, and from e1 on for the partners) and its first pair.
   const int P = p.pairs, rot = 2 * P * p.axes;
   int e0 = u * V, e1 = 0, pair = e0 / 2, axis = 0;
-  bool turned = e0 < rot;
+  bool turns = e0 < rot;
   if constexpr (!INTER) {
     const int per = P / V, nt = per * p.axes;   // units of pairs per axis, in all
-    turned = u < nt;
-    if (turned) {
+    turns = u < nt;
+    if (turns) {
       axis = u >= per ? 1 : 0;
       pair = (u - axis * per) * V;
       e0 = axis * 2 * P + pair;
@@ -129,7 +133,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
 
   const int np = P * p.axes - pair;   // (interleaved: the pairs of the unit that are turned)
   float cs[NP], sn[NP];
-  if (turned) {
+  if (turns) {
     int r, c;
     sl.position(p, n, r, c);
 #pragma unroll
@@ -150,7 +154,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
     const int m = min(kBatch, s1 - s);
     sl.rows(p, m, n, src, dst);
     auto put = [](T *q, const auto &v) { rope_put<THROUGH>(q, v); };
-    if (!INTER && !turned) {
+    if (!INTER && !turns) {
       tail x[kBatch];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j)
@@ -170,18 +174,18 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       if (j >= m) break;
-      if (!INTER || turned) {
+      if (!INTER || turns) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
           if constexpr (INTER) {
             const T t1 = a[j][2 * i], t2 = a[j][2 * i + 1];
             const float x1 = (float)t1, x2 = (float)t2;
-            a[j][2 * i] = !MIXED || i < np ? (T)(x1 * cs[i] - x2 * sn[i]) : t1;
-            a[j][2 * i + 1] = !MIXED || i < np ? (T)(x2 * cs[i] + x1 * sn[i]) : t2;
+            a[j][2 * i] = !MIXED || i < np ? (T)turned(x1, x2, cs[i], -sn[i]) : t1;
+            a[j][2 * i + 1] = !MIXED || i < np ? (T)turned(x2, x1, cs[i], sn[i]) : t2;
           } else {
             const float x1 = (float)a[j][i], x2 = (float)c[j][i];
-            a[j][i] = (T)(x1 * cs[i] - x2 * sn[i]);
-            c[j][i] = (T)(x2 * cs[i] + x1 * sn[i]);
+            a[j][i] = (T)turned(x1, x2, cs[i], -sn[i]);
+            c[j][i] = (T)turned(x2, x1, cs[i], sn[i]);
           }
         }
       }
@@ -231,7 +235,7 @@ __global__ void __launch_bounds__(kThreads) rope_chunks(RopeArgs p) {
       sn[i] *= s;
     }
   }
-  const int turned = rot - u * V;
+  const int count = rot - u * V;   // features that are turned
   for (int s = sl.s0; s < sl.s1; s += kBatch) {
     const T *src[kBatch];
     T *dst[kBatch];
@@ -254,7 +258,7 @@ __global__ void __launch_bounds__(kThreads) rope_chunks(RopeArgs p) {
       for (int i = 0; i < V; ++i) {
         const T x = a[j][i];
         const float y = (float)part[other[i]];
-        a[j][i] = i < turned ? (T)((float)x * cs[i] + y * sn[i]) : x;
+        a[j][i] = i < count ? (T)turned((float)x, y, cs[i], sn[i]) : x;
       }
       rope_put<THROUGH>(dst[j] + u * V, a[j]);
     }

@@ -129,6 +129,38 @@ def test_long_rows(d, pairs, interleaved, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+# pairs that fill accesses, in halves and interleaved; chunks; pairs beside features to copy;
+# rows too long for chunks, by the pair and by the access
+@pytest.mark.parametrize("d,pairs,interleaved", [(64, 32, False), (64, 32, True), (64, 13, False), (64, 13, True),
+                                                 (1032, 13, False), (1032, 64, False)], ids=str)
+@pytest.mark.parametrize("where", ["shared", "per batch", "grid"])
+def test_more_than_the_caches_hold(d, pairs, interleaved, dtype, where):
+    """Calls that move more than 256 MB, with runs of heads that cross batch elements: the
+    bits of calls on pieces of the sequence, and rows of them against float64."""
+    B, heads, kv = 3, 11, 2
+    N = (1 << 27) // (B * (heads + kv) * d * dtype.itemsize) + 13
+    assert 2 * B * (heads + kv) * N * d * dtype.itemsize > 256 << 20
+    g = torch.Generator(device="cuda").manual_seed(14)
+    q, k = (torch.randn(B, h, N, d, generator=g, device="cuda").to(dtype) for h in (heads, kv))
+    kw = dict(interleaved=interleaved, grid_w=0)
+    pos = torch.randperm(N, generator=g, device="cuda").to(torch.int32)
+    if where == "per batch":
+        pos = torch.stack([pos, pos.flip(0), pos * 3])
+    elif where == "grid":
+        kw["grid_w"], pairs = 131, pairs // 2
+    freqs, _ = hla.rope_freqs(pairs)
+    q2, k2 = hla.rope(q, freqs, k=k, pos=pos, **kw)
+    edges = [0, N // 3, N // 3 + 1, N - 8, N]
+    for a, b in zip(edges, edges[1:]):
+        q3, k3 = hla.rope(q[:, :, a:b], freqs, k=k[:, :, a:b], pos=pos[..., a:b].contiguous(), **kw)
+        assert torch.equal(q2[:, :, a:b], q3) and torch.equal(k2[:, :, a:b], k3), (a, b)
+    rows = torch.tensor([0, 1, N // 2, N - 2, N - 1], device="cuda")
+    check(q2[:, :, rows], q[:, :, rows], freqs, pos=pos[..., rows], **kw)
+    check(k2[:, :, rows], k[:, :, rows], freqs, pos=pos[..., rows], **kw)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_infinity_stays_in_its_pair(interleaved):
     freqs, _ = hla.rope_freqs(5)
