@@ -364,6 +364,69 @@ def test_large_values(size, dtype):
     assert bool(out.isfinite().all())
 
 
+def cus():
+    return torch.cuda.get_device_properties(0).multi_processor_count
+
+
+def work_bytes(size, dtype, backward):
+    n = ctypes.c_int64()
+    code = hla.HLA_BF16 if dtype is BF else hla.HLA_F32
+    assert hla.lib().hla_cross_attn_workspace(*size, code, backward, ctypes.byref(n)) == hla.HLA_OK
+    return n.value
+
+
+def check_pairs(size, lengths, dtype, seed, pairs):
+    """A step, with NaN in the states that are not seen: some (batch, key head) pairs, each
+    on its own, against float64, and no other result NaN or infinite."""
+    B, H, kv, N, M, d = size
+    G = H // kv
+    q, k, v, dout = inputs(*size, dtype, seed=seed)
+    n = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    for b, x in enumerate(lengths or ()):
+        k[b, :, x:] = v[b, :, x:] = float("nan")
+    out, lse = hla.cross_attn_fwd(q, k, v, n)
+    grads = hla.cross_attn_bwd(q, k, v, out, dout, lse, n)
+    for b, t in pairs:
+        one, hs, ts = slice(b, b + 1), slice(t * G, t * G + G), slice(t, t + 1)
+        ref = reference(q[one, hs], k[one, ts], v[one, ts], None if n is None else n[one], d ** -0.5, dout[one, hs])
+        for name, got, heads in zip(("out", "lse", "dq", "dk", "dv"), (out, lse, *grads), (hs, hs, hs, ts, ts)):
+            compare(name, got[one, heads], ref)
+    assert all(bool(g.isfinite().all()) for g in (out, *grads))
+    assert torch.equal(lse.isfinite().all(2).all(1).cpu(),
+                       torch.tensor([x > 0 for x in lengths] if lengths else [True] * B))
+
+
+# Tiles of 128 rows (as many as there are CUs, and keys that do not stay in LDS), several
+# key tiles, ragged at both ends: below, at and above the 256 keys up to which delta is put
+# right, with elements that see none; shared heads; and dk and dv in tiles of 128 keys, the
+# rows split (the first three) or not (the last)
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("size,lengths", [
+    ((4, 2, 2, 4001, 321, 64), None), ((4, 2, 2, 4001, 321, 64), [321, 257, 256, 129]),
+    ((4, 2, 2, 4001, 321, 32), [0, 1, 65, 320]), ((2, 8, 2, 2050, 700, 64), [700, 333]),
+    ((2, 8, 2, 2050, 700, 32), None), ((8, 8, 8, 400, 300, 64), [300, 0, 1, 299, 128, 129, 257, 64]),
+    ((8, 8, 8, 400, 300, 32), None)], ids=str)
+def test_many_rows(size, lengths, dtype):
+    B, H, kv, N, M, d = size
+    rows = B * kv * ((H // kv * N + 127) // 128)
+    assert M > 128 and rows >= cus(), "tiles of 128 rows"
+    parts = 2 * B * kv * ((M + 127) // 128) <= cus()
+    stats = 8 * B * kv * ((H // kv * N + 127) // 128 * 128)
+    assert (work_bytes(size, dtype, 1) > stats) == parts and parts == (size[0] < 8)
+    check_pairs(size, lengths, dtype, 31, [(0, 0), (1, kv - 1), (B - 2, 1), (B - 1, 0)])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lengths", [None, [130, 1, 0, 129, 64, 128, 127, 130, 33, 0, 100]], ids=["all", "ragged"])
+def test_two_workgroups_per_cu_for_dk_and_dv(lengths):
+    """Heads of 32 in bf16 with rows enough that the splits of dk and dv take twice as many
+    workgroups as there are CUs."""
+    size = (11, 4, 4, 6000, 130, 32)
+    assert work_bytes(size, BF, 1) == 8 * 44 * 6016 + 2 * cus() * 128 * 8 * 32
+    check_pairs(size, lengths, BF, 32, [(0, 0), (3, 1), (5, 2), (10, 3)])
+
+
 class Raw:
     """The C entries on made-up addresses: every call here must be refused."""
     Q, K, V, O, L, W, G, DQ, DK, DV, N = (0x10000000 * i for i in range(1, 12))

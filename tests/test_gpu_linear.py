@@ -159,6 +159,37 @@ def test_tiles_for_every_cu(size):
 
 
 @pytest.mark.gpu
+def test_weight_gradients_in_wide_tiles():
+    """dw in 256 x 256 tiles that fill the CUs, the last column of them and the tokens
+    ragged (as many tiles of 256 as there are CUs)."""
+    x, w, b, r, dy = make(200, 4088, 4096, BF, seed=9)
+    _, pre = hla.linear(x, w, b, act="gelu", with_pre=True)
+    dx, dw, db = hla.linear_bwd(x, w, dy, pre, act="gelu", with_bias=True)
+    check_backward(x, w, dy, pre, "gelu", dx, dw, db)
+
+
+@pytest.mark.gpu
+def test_weight_gradients_in_parts_of_wide_tiles():
+    """dw in 256 x 256 tiles, the tokens in four parts, everything ragged. Rows of dx and of
+    dw, each on its own, against float64."""
+    T, K, F = 8200, 1016, 4088
+    x, w, b, r, dy = make(T, K, F, BF, seed=10)
+    n = ctypes.c_int64()
+    assert hla.lib().hla_linear_workspace(T, K, F, 0, hla.HLA_BF16, 1, ctypes.byref(n)) == hla.HLA_OK
+    tiles = ((K + 255) // 256) * ((F + 255) // 256)
+    parts = torch.cuda.get_device_properties(0).multi_processor_count // tiles
+    assert parts > 1 and parts * K * F * 4 <= n.value < (parts + 1) * K * F * 4
+    y, pre = hla.linear(x, w, b, act="gelu", residual=r, with_pre=True)
+    dx, dw, db = hla.linear_bwd(x, w, dy, pre, act="gelu", with_bias=True)
+    ts = torch.cat([torch.arange(0, T, 97), torch.arange(T - 9, T)]).cuda()
+    fs = torch.cat([torch.arange(0, F, 89), torch.arange(F - 9, F)]).cuda()
+    check_forward(x[ts], w, b, r[ts], "gelu", y[ts], pre[ts])
+    check_backward(x[ts], w, dy[ts], pre[ts], "gelu", dx[ts], None, None)
+    check_backward(x, w[fs], dy[:, fs], pre[:, fs], "gelu", None, dw[fs], db[fs])
+    assert all(bool(t.isfinite().all()) for t in (y, pre, dx, dw, db))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 def test_some_gradients_only(dtype):
     T, K, F = 150, 64, 96
