@@ -650,11 +650,15 @@ uint32_t set_plan(GemmArgs &p, const Plan &plan) {
   return (uint32_t)(na * nb * plan.splits);
 }
 
+// (A layer's larger tiles are taken where they are more than half of the workgroups
+// that plan_of counts on, so they are never in parts.)
 template <typename T, bool AT, bool BT, int EPI>
 hipError_t launch_gemm(GemmArgs &p, const Plan &plan, hipStream_t s) {
   const dim3 grid(set_plan(p, plan));
   if constexpr (sizeof(T) == 4) {
     hipLaunchKernelGGL((gemm_kernel<T, 64, 64, 2, 2, 128, 2, AT, BT, EPI>), grid, dim3(256), 0, s, p);
+  } else if constexpr (EPI == EPI_PART && !AT) {
+    hipLaunchKernelGGL((gemm_kernel<T, 64, 64, 2, 2, 128, 4, AT, BT, EPI>), grid, dim3(256), 0, s, p);
   } else {
     if (plan.tile == 256) {
       hipLaunchKernelGGL((gemm_kernel<T, 256, 256, 4, 2, 128, 2, AT, BT, EPI>), grid, dim3(512), 0, s, p);

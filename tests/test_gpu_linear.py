@@ -189,6 +189,41 @@ def test_weight_gradients_in_parts_of_wide_tiles():
     assert all(bool(t.isfinite().all()) for t in (y, pre, dx, dw, db))
 
 
+# dw in 128 x 128 tiles, whole; dx in 256 x 256 tiles, the features in parts
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [(304, 2000, 3000), (2050, 2040, 8200)], ids=str)
+def test_gradients_in_tiles_of_other_shapes(size):
+    T, K, F = size
+    x, w, b, r, dy = make(*size, BF, seed=11)
+    _, pre = hla.linear(x, w, b, act="silu", with_pre=True)
+    dx, dw, db = hla.linear_bwd(x, w, dy, pre, act="silu", with_bias=True)
+    ts = torch.cat([torch.arange(0, T, 31), torch.arange(T - 9, T)]).cuda()
+    fs = torch.cat([torch.arange(0, F, 61), torch.arange(F - 9, F)]).cuda()
+    check_backward(x[ts], w, dy[ts], pre[ts], "silu", dx[ts], None, None)
+    check_backward(x, w[fs], dy[:, fs], pre[:, fs], "silu", None, dw[fs], db[fs])
+    assert all(bool(t.isfinite().all()) for t in (dx, dw, db))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("size,keep", [((150, 64, 4096), 0), ((4096, 64, 96), 1)], ids=["dx", "dw"])
+def test_one_gradient_in_parts(size, keep, dtype):
+    """dx or dw alone, its contraction in parts: the bits of the call for all three."""
+    T, K, F = size
+    x, w, b, r, dy = make(*size, dtype, seed=12)
+    n, code = ctypes.c_int64(), hla._dtype_code(x)
+    assert hla.lib().hla_linear_workspace(T, K, F, 0, code, 1, ctypes.byref(n)) == hla.HLA_OK
+    want = hla.linear_bwd(x, w, dy)[keep]
+    assert n.value >= 2 * want.numel() * 4, "parts"
+    got, work = torch.full_like(want, 7.0), torch.empty(n.value, dtype=torch.uint8, device="cuda")
+    args = [got.data_ptr() if i == keep else 0 for i in range(3)]
+    st = hla.lib().hla_linear_bwd(x.data_ptr(), w.data_ptr(), 0, dy.data_ptr(), 0, *args, T, K, F, code,
+                                  work.data_ptr(), n.value, hla._stream(x))
+    assert st == hla.HLA_OK, hla.lib().hla_last_error()
+    check_backward(x, w, dy, None, "none", got if keep == 0 else None, got if keep == 1 else None, None)
+    assert torch.equal(got, want)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 def test_some_gradients_only(dtype):
