@@ -427,6 +427,31 @@ def test_two_workgroups_per_cu_for_dk_and_dv(lengths):
     check_pairs(size, lengths, BF, 32, [(0, 0), (3, 1), (5, 2), (10, 3)])
 
 
+# a token and its key splits, few rows, keys that stay in LDS, many rows
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("N,M", [(1, 1100), (70, 1100), (200, 100), (33000, 300)])
+def test_rows_that_lie_far_apart(N, M, dtype):
+    """States 16 MiB apart (in one tensor, heads side by side) and queries over some 8 GiB:
+    offsets past 32 bits in every input and output; the bits of the dense call."""
+    B, H, kv, d = 1, 2, 1, 64
+    q, k, v, dout = inputs(B, H, kv, N, M, d, dtype, seed=41)
+    n = torch.tensor([M - 3], dtype=torch.int32, device="cuda")
+    want, lse = hla.cross_attn_fwd(q, k, v, n)
+    grads = hla.cross_attn_bwd(q, k, v, want, dout, lse, n)
+    far, near = 2 ** 24 // dtype.itemsize, min(2 ** 25, 2 ** 33 // N // dtype.itemsize // 1024 * 1024)
+    states = torch.empty(M * far, dtype=dtype, device="cuda")
+    rows = torch.empty(N * near, dtype=dtype, device="cuda")
+    k2, v2, dk, dv = (states[256 * i:].as_strided((B, kv, M, d), (M * far, d, far, 1)) for i in range(4))
+    q2, out, dout2, dq = (rows[256 * i:].as_strided((B, H, N, d), (N * near, d, near, 1)) for i in range(4))
+    for to, t in ((q2, q), (k2, k), (v2, v), (dout2, dout)):
+        to.copy_(t)
+    got, lse2 = hla.cross_attn_fwd(q2, k2, v2, n, out=out)
+    assert torch.equal(got, want) and torch.equal(lse2, lse)
+    for a, b in zip(hla.cross_attn_bwd(q2, k2, v2, got, dout2, lse2, n, dq=dq, dk=dk, dv=dv), grads):
+        assert torch.equal(a, b)
+
+
 class Raw:
     """The C entries on made-up addresses: every call here must be refused."""
     Q, K, V, O, L, W, G, DQ, DK, DV, N = (0x10000000 * i for i in range(1, 12))

@@ -225,6 +225,26 @@ def test_one_gradient_in_parts(size, keep, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("K,F", [(8, 8192), (8192, 8)])
+def test_more_results_than_32_bits_count(K, F):
+    """x or y of 4.9e9 elements: rows at the ends and around element 2^32."""
+    T = 600000
+    g = torch.Generator(device="cuda").manual_seed(13)
+
+    def normal(*shape, std=1.0):
+        return torch.empty(shape, dtype=BF, device="cuda").normal_(0, std, generator=g)
+    x, w, b, dy = normal(T, K), normal(F, K, std=K ** -0.5), normal(F), normal(T, F)
+    y, pre = hla.linear(x, w, b, act="silu", with_pre=True)
+    mid = 2 ** 32 // max(K, F)
+    ts = torch.cat([torch.arange(0, 9), torch.arange(mid - 5, mid + 5), torch.arange(T - 9, T)]).cuda()
+    check_forward(x[ts], w, b, None, "silu", y[ts], pre[ts])
+    dx, dw, db = hla.linear_bwd(x, w, dy, pre, act="silu", with_bias=True)
+    check_backward(x[ts], w, dy[ts], pre[ts], "silu", dx[ts], None, None)
+    fs, ks = torch.tensor([0, F // 2, F - 1]).cuda(), torch.tensor([0, K // 2 + 1, K - 1]).cuda()
+    check_backward(x[:, ks], w[fs][:, ks], dy[:, fs], pre[:, fs], "silu", None, dw[fs][:, ks], db[fs])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 def test_some_gradients_only(dtype):
     T, K, F = 150, 64, 96

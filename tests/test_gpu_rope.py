@@ -161,6 +161,22 @@ def test_more_than_the_caches_hold(d, pairs, interleaved, dtype, where):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("pairs,interleaved", [(32, False), (13, False), (13, True)])
+def test_rows_that_lie_far_apart(pairs, interleaved):
+    """Rows 64 MiB apart, heads side by side: offsets past 32 bits; the bits of the dense call."""
+    N, far = 150, 2 ** 25
+    freqs, _ = hla.rope_freqs(pairs)
+    q, k = normal((1, 3, N, 64), torch.bfloat16, 15), normal((1, 1, N, 64), torch.bfloat16, 16)
+    want = hla.rope(q, freqs, k=k, interleaved=interleaved)
+    t = torch.empty(N * far, dtype=torch.bfloat16, device="cuda")
+    q2, k2, q3, k3 = (t[256 * i:].as_strided((1, h, N, 64), (N * far, 64, far, 1)) for i, h in enumerate((3, 1, 3, 1)))
+    q2.copy_(q)
+    k2.copy_(k)
+    got = hla.rope(q2, freqs, k=k2, interleaved=interleaved, q_out=q3, k_out=k3)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_infinity_stays_in_its_pair(interleaved):
     freqs, _ = hla.rope_freqs(5)
