@@ -540,6 +540,8 @@ hla_status hla_cross_attn_workspace(int64_t B, int64_t heads, int64_t kv_heads, 
 /*
  * Token-wise linear layer with bias, activation and residual in its epilogue:
  *   z = x W^T + bias,  y = act(z) + residual
+ * (The layers that lead into and out of the attention's [B, heads, N, d], with a change of
+ * the tokens' order, are hla_qkv_proj, hla_out_proj and their _perm forms.)
  * x: [T, K], w: [F, K] (row f is output feature f), bias: [F] or NULL, residual:
  * [T, F] or NULL, y: [T, F], all of dtype, contiguous. pre: [T, F] or NULL, receives z
  * (rounded to dtype), which the backward of an activation needs. residual may be y

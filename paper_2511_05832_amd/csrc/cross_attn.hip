@@ -26,9 +26,11 @@
 // in order by a third launch).
 //
 // What bounds them, in heads of 64 with many rows and keys: a wave's exponentials and its
-// matrix products follow one another, at the two or three waves per SIMD that registers and
-// rows allow. 8 heads on 2, 4096 rows and keys, batch 2, bf16: forward 117 us (590 TFLOP/s),
-// dq 130 (790), dk and dv 151 (910).
+// matrix products follow one another, and too few waves stand beside it: 512 workgroups of
+// four are two to a SIMD, 1.6 of them resident over the launch (1.2 where lengths are ragged).
+// 8 heads on 2, 4096 rows and keys, batch 2, bf16, by the clock: forward 101 to 117 us (590
+// to 680 TFLOP/s; vector issue 49%, matrix cores 26%), dq 115 to 130 (790 to 890; 48, 36%), dk
+// and dv 139 to 153 (900 to 990; 46, 42%).
 //
 // Masked places: keys from length on are never loaded (the last tile's copies stop at
 // the last seen key, of which the others are copies) and get weight 0, so nothing that
@@ -294,8 +296,8 @@ __global__ void __launch_bounds__(256, 2) cross_fwd(CrossArgs a) {
 // LDS); the keys may be split over workgroups as well, a.per of them each, so that the
 // splits of a long and a short batch element are of one size and those past its end do
 // nothing. Bound by the states' bytes: 128 KiB per CU are in flight. One token of 16
-// heads against 4096 states of 4, batch 16 of lengths 2048 to 4096: 12 us and 4 to join
-// (50 MB, 3.2 TB/s).
+// heads against 4096 states of 4, batch 16 of lengths 2048 to 4096 (50 MB): 13.7 us from
+// memory (3.7 TB/s), 11.9 where the caches hold the states, and 4 to join.
 template <typename T, int D>
 struct FewRows {
   using Tl = Tile<T, D>;
@@ -431,8 +433,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) cross_fwd_few(Cro
 
 // Up to 128 keys (a text's tokens): keys and values stay in LDS, and a workgroup's waves,
 // each for itself, go through blocks of 32 rows with the next block's queries in flight.
-// Bound by HBM (q in, out out): 16 x 6 heads of 32, 4096 rows against 77 keys 16 us (3.2
-// TB/s; 645 as elementary operations); 4 x 8 heads of 64, 16384 rows 39 us (3.4 TB/s).
+// Bound by a block's latency: its loads, products and stores follow one another, with one
+// block ahead and 1.5 waves per SIMD (vector issue 36%). 16 x 6 heads of 32, 4096 rows
+// against 77 keys 19.3 us from memory (2.6 TB/s), 18.4 over one set of inputs (645 as
+// elementary operations); 4 x 8 heads of 64, 16384 rows 39.5 (3.4 TB/s) and 35.8.
 // Workgroups per CU of the kernels whose keys stay in LDS: what their registers (three,
 // two for rows of 128 bytes) or LDS (fp32 rows of 64: 98 KiB, one) leave.
 constexpr int short_waves(int row_bytes) { return row_bytes > 128 ? 1 : (row_bytes > 64 ? 2 : 3); }
@@ -799,8 +803,8 @@ __device__ __forceinline__ int splits_of(const CrossArgs &a, int tiles) {
 // w / KB of the rows of every step (RB blocks of 32 each). Rows come into an LDS ring by
 // the 16-byte DMA; the halves are added through LDS at the end. Bound by the waves' vector
 // and matrix work, two waves per SIMD (200 registers): 4096 rows of 8 heads on 2 against
-// 4096 keys, batch 2, heads of 64 in bf16: 151 us (910 TFLOP/s); with 64 keys to a
-// workgroup, and twice the rows' traffic, the whole backward takes 13 us longer.
+// 4096 keys, batch 2, heads of 64 in bf16: 139 to 153 us (900 to 990 TFLOP/s); with 64 keys
+// to a workgroup, and twice the rows' traffic, the whole backward takes 13 us longer.
 template <typename T, int D, int KB, int RB>
 __global__ void __launch_bounds__(128 * KB, 2) cross_dkdv(CrossArgs a) {
   using Tl = Tile<T, D>;

@@ -192,9 +192,10 @@ __device__ __forceinline__ void finish(const GemmArgs &p, float (&z)[Type<T>::V]
 // Output tiles of TB rows by TA columns by WA x WB waves, a ring of RING stages of KB
 // bytes of every row, filled by the 16-byte LDS DMA. What bounds it, in 256 x 256 tiles:
 // the matrix cores and the LDS reads that feed them, about alike, then the stores, which
-// one workgroup per CU does not hide. 16384 x 4096 results in bf16: 97 us per 1000
-// contracted elements (1.38 PFLOP/s) and 36 us besides; with bias and gelu 14 to 18 us
-// more, and with the residual and the stored pre-activation 32 (403 MB in all).
+// one workgroup per CU does not hide. 16384 x 4096 results in bf16, over one set of inputs:
+// 97 us per 1000 contracted elements (1.38 PFLOP/s) and 36 to 39 us besides; with bias and
+// gelu 18 us more, and with the residual and the stored pre-activation 37 (403 MB in all).
+// From memory the three take 172, 184 and 198 us, 139, 157 and 176 over one set.
 template <typename T, int TA, int TB, int WA, int WB, int KB, int RING>
 struct Shape {
   static constexpr int PITCH = TA + 4;   // floats of a staged output row
@@ -368,8 +369,8 @@ __global__ void __launch_bounds__(256, 2) gemm_pair_kernel(GemmArgs dx, GemmArgs
 // takes 16 features, its waves share the contraction in runs of 128 bytes a row; rows
 // of W go from memory into operands of the 16 x 16 products (A = features, B = tokens),
 // 1 KiB per load, with no stop in LDS. The waves' sums are added through LDS. 4 tokens,
-// 2048 -> 8192, bf16, weights from memory: 10.2 us (3.3 TB/s); with 4 waves and the same
-// loads in flight per wave 12.6, with 16 waves 12.0.
+// 2048 -> 8192, bf16: 10.5 us with the weights from memory (3.2 TB/s), 8.2 where the caches
+// hold them; with 4 waves and the same loads in flight per wave 2.4 more, with 16 waves 1.8.
 constexpr int kFewWaves = 8;
 template <typename T>
 struct Few;
@@ -462,7 +463,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) few_kernel(GemmArgs p) {
 // dz = dy act'(z) (when `dz` is given), and partial column sums of dz for the bias: a
 // workgroup takes 32 chunks of columns by a run of rows. Where one run holds them all the
 // sums are the bias' gradient itself (`db`), which saves the adding launch. Bound by HBM:
-// 16384 x 4096, gelu, bf16 82 us (4.9 TB/s).
+// 16384 x 4096, gelu, bf16 72 us (5.6 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(256) dz_kernel(const T *dy, const T *pre, T *dz, float *sums, T *db, int T_,
                                                  int F, int rows, int act) {

@@ -7,9 +7,10 @@
 // the pairs of a 16-byte access or two, or features to copy - at one position, computes the
 // unit's sines and cosines once, and goes through a run of (batch, head) slices with
 // them, so the trigonometry (about 60 operations per pair) is shared. The runs leave the
-// chip 32 waves per CU, two slices' loads in flight each. Measured: 64x64 layer, 6 heads
-// of 32, batch 16, bf16 18 us (5.6 TB/s); 65536 tokens, 8 + 2 heads of 64, fp32 63 us
-// (5.3 TB/s; a copy of 1 GiB 5.1).
+// chip 32 waves per CU, two slices' loads in flight each. Measured, from memory / over one
+// set of inputs, which the caches hold in part: 64x64 layer, 6 heads of 32, batch 16, bf16
+// 23.6 / 18.0 us (4.3 / 5.6 TB/s); 65536 tokens, 8 + 2 heads of 64, fp32 63.5 / 51.4 us (5.3 /
+// 6.5 TB/s; a copy of 1 GiB 5.1).
 // Results go past the caches where a call moves more than they hold (256 MB; the fp32
 // case 65.9 -> 64.7 us, the units' kernel 77 -> 70), while at 84 MB 16.4 -> 18.4 and the
 // next kernel would find its inputs in memory.
@@ -198,7 +199,8 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
 // Halves by chunks: a thread owns 16 bytes of a row, whatever they hold, and finds its
 // features' partners where the row's other chunks, held by the same wave, have put them
 // in LDS. Features to copy stay as they are. 12 slices of 44540 rows of 64, bf16,
-// 26 pairs on a grid: 31 us (4.4 TB/s); as units of one pair, 2 bytes an access, 58.
+// 26 pairs on a grid: 34 us from memory (4.0 TB/s), 29 over one set of inputs; as units of
+// one pair, 2 bytes an access, 58.
 template <typename T, bool THROUGH>
 __global__ void __launch_bounds__(kThreads) rope_chunks(RopeArgs p) {
   constexpr int V = 16 / (int)sizeof(T);
