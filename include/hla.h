@@ -557,7 +557,8 @@ hla_status hla_cross_attn_workspace(int64_t B, int64_t heads, int64_t kv_heads, 
  * which is slower and sums in another order. Calls whose work overlaps in time need one
  * each.
  * Any T >= 1; K and F multiples of 8 (bf16) or 4 (f32), below 2^20; T up to 2^30; with
- * each rounded up to 64, T * max(K, F) and K * F up to 2^36 - 2^14; otherwise UNSUPPORTED.
+ * each rounded up to 64, T * max(K, F) and, for the backward, K * F up to 2^36 - 2^14;
+ * otherwise UNSUPPORTED.
  */
 typedef enum {
   HLA_ACT_NONE = 0,

@@ -358,7 +358,7 @@ struct Tensor {
   int64_t bytes;
 };
 
-hla_status linear_sizes(int64_t T, int64_t K, int64_t F, hla_act act, hla_dtype dtype, LinearArgs *a) {
+hla_status linear_sizes(int64_t T, int64_t K, int64_t F, hla_act act, hla_dtype dtype, bool backward, LinearArgs *a) {
   const int64_t es = dtype_size(dtype);
   if (!es) return fail(HLA_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
   if (act < HLA_ACT_NONE || act > HLA_ACT_SILU) return fail(HLA_ERR_INVALID_ARG, "unknown activation %d", (int)act);
@@ -371,8 +371,8 @@ hla_status linear_sizes(int64_t T, int64_t K, int64_t F, hla_act act, hla_dtype 
   // (a launch counts its threads in 32 bits: below 2^24 workgroups of 256, one to a tile of
   // 64 x 64; larger tiles have up to 512 threads, and are at most half as many)
   const int64_t t = (T + 63) / 64, k = (K + 63) / 64, f = (F + 63) / 64, most = (1 << 24) - 4;
-  if (t * std::max(k, f) > most || k * f > most)
-    return fail(HLA_ERR_UNSUPPORTED, "T * max(K, F) or K * F, in tiles of 64 x 64, is not below 2^36");
+  if (t * std::max(k, f) > most || (backward && k * f > most))
+    return fail(HLA_ERR_UNSUPPORTED, "T * max(K, F), or K * F of a backward, in tiles of 64 x 64, is not below 2^36");
   *a = {};
   a->T = (int32_t)T;
   a->K = (int32_t)K;
@@ -418,7 +418,7 @@ hla_status hla_linear(const void *x, const void *w, const void *bias, const void
                       hla_act act, void *y, void *pre, int64_t T, int64_t K, int64_t F,
                       hla_dtype dtype, void *work, int64_t work_bytes, hla_stream_t stream) {
   LinearArgs a;
-  hla_status st = linear_sizes(T, K, F, act, dtype, &a);
+  hla_status st = linear_sizes(T, K, F, act, dtype, false, &a);
   if (st != HLA_OK) return st;
   if (!x || !w || !y) return fail(HLA_ERR_INVALID_ARG, "%s is NULL", !x ? "x" : (!w ? "w" : "y"));
   const int64_t es = dtype_size(dtype);
@@ -445,7 +445,7 @@ hla_status hla_linear_workspace(int64_t T, int64_t K, int64_t F, hla_act act, hl
                                 int32_t backward, int64_t *bytes) {
   LinearArgs a;
   if (!bytes) return fail(HLA_ERR_INVALID_ARG, "bytes is NULL");
-  hla_status st = linear_sizes(T, K, F, act, dtype, &a);
+  hla_status st = linear_sizes(T, K, F, act, dtype, backward != 0, &a);
   if (st != HLA_OK) return st;
   a.dx = a.dw = a.db = bytes;   // (all of them; the addresses are not used)
   a.parts = true;
@@ -458,7 +458,7 @@ hla_status hla_linear_bwd(const void *x, const void *w, const void *pre, const v
                           int64_t F, hla_dtype dtype, void *work, int64_t work_bytes,
                           hla_stream_t stream) {
   LinearArgs a;
-  hla_status st = linear_sizes(T, K, F, act, dtype, &a);
+  hla_status st = linear_sizes(T, K, F, act, dtype, true, &a);
   if (st != HLA_OK) return st;
   if (!dx && !dw && !db) return fail(HLA_ERR_INVALID_ARG, "dx, dw and db are all NULL");
   if (!dy) return fail(HLA_ERR_INVALID_ARG, "dy is NULL");

@@ -455,8 +455,8 @@ def test_tensors_are_checked_before_the_workspace():
     assert st == INV and "dw overlaps dx" in hla.lib().hla_last_error().decode()
 
 
-@pytest.mark.parametrize("T,K,F", [(1 << 30, 8, 8), (1 << 30, 8, 64), (1 << 26, 1024, 8), (1 << 26, 8, 1024),
-                                   (128, (1 << 20) - 8, (1 << 20) - 8)], ids=str)
+@pytest.mark.parametrize("T,K,F", [(1 << 30, 8, 8), (1 << 30, 8, 64), (1 << 26, 1024, 8), (1 << 26, 8, 1024)],
+                         ids=str)
 @pytest.mark.parametrize("dtype", [hla.HLA_BF16, hla.HLA_F32])
 def test_more_workgroups_than_a_launch_holds(T, K, F, dtype):
     """A launch counts its threads in 32 bits: 2^24 workgroups of 256 are too many."""
@@ -465,6 +465,9 @@ def test_more_workgroups_than_a_launch_holds(T, K, F, dtype):
         st = hla.lib().hla_linear_workspace(T, K, F, 2, dtype, backward, ctypes.byref(n))
         assert st == UNS and "2^36" in hla.lib().hla_last_error().decode()
     assert hla.lib().hla_linear_workspace((1 << 30) - 256, 8, 64, 2, dtype, 1, ctypes.byref(n)) == hla.HLA_OK
+    wide = (1 << 20) - 8   # (the weights' gradient)
+    for backward, want in ((0, hla.HLA_OK), (1, UNS)):
+        assert hla.lib().hla_linear_workspace(128, wide, wide, 2, dtype, backward, ctypes.byref(n)) == want
 
 
 def test_refusals_of_the_binding():
